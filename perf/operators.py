@@ -1,0 +1,413 @@
+"""The 8-bit key/value cache's operators, as cases that can be timed: their plain form and the package's kernels.
+
+A model that reads the tokens a backbone kept (a decoder behind it, or a reader that attends across) holds their
+keys and values, and those of what it writes itself, from call to call.  Four operators do that:
+
+  append   new keys and values enter the cache: rounded to 8 bits, with one scale for `block` tokens of a head
+  attend   queries attend to what the cache holds; the weight that every held token gets may be added up
+  evict    the tokens with the least weight leave, the rest moves together into another cache
+  read     tokens' values again, as the cache holds them
+
+`own` chooses between the plain form, elementary operations in 32 bits, and the calls of
+`paper_2601_12150_amd.binding`.  An append and an eviction return what the caches then hold, so they read it back.
+
+The cache holds a value x as code * scale.  Scales are powers of two, the smallest s with max |x| <= 127 s (int8) or
+448 s (e4m3) over the block: x / s is exact, and which code is nearest (ties to the even one) does not depend on how it
+is computed.  A block that already holds tokens keeps its scale unless a new one needs more; then its codes are rounded
+again, to the larger scale.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+CODES = {"i8": (torch.int8, 127), "e4m3": (torch.float8_e4m3fn, 448)}
+
+
+def listed():
+    return [
+        # ---- append
+        # one token of one sequence in fp32, in the middle of a block: the smallest call
+        _append("append_1_f32_i8", "f32", "i8", 1, 16, 64, 64, 512, 1, 413),
+        # a step of 32 sequences, each at a place of its own
+        _append("append_1_b32_bf16_e4m3", "bf16", "e4m3", 32, 8, 128, 32, 256, 1, 255),
+        # prompts of up to 4001 tokens in a padded batch, behind 37 held tokens
+        _append("append_4001_b4_bf16_i8", "bf16", "i8", 4, 8, 128, 64, 4096, 4001, 4038),
+        # ---- attend
+        # one query over a small image's 576 tokens (24 x 24) and a short text, each head with its own keys: latency
+        _attend("attend_1_f32_i8", "f32", "i8", 1, 16, 1, 64, 64, 640, 1, 613),
+        # a step of 32 sequences of up to 4000 tokens, one slot of them empty
+        _attend("attend_1_b32_bf16_i8", "bf16", "i8", 32, 8, 4, 128, 64, 4096, 1, 4000),
+        # one long sequence, with the weights that a later eviction goes by
+        _attend("attend_1_long_bf16_e4m3_w", "bf16", "e4m3", 1, 8, 4, 128, 128, 131072, 1, 131001, weights=True),
+        # four drafted tokens a sequence, groups of eight heads, with weights
+        _attend("attend_4_b8_bf16_e4m3_w", "bf16", "e4m3", 8, 8, 8, 128, 32, 16384, 4, 16000, weights=True),
+        # prompts: 2 sequences of up to 4096 tokens
+        _attend("attend_4096_b2_bf16_i8", "bf16", "i8", 2, 8, 4, 128, 64, 4096, 4096, 4096),
+        # 512 queries (a reader's own latents) across a 2048-pixel image's 16385 tokens, all of them visible, with weights
+        _attend("attend_512_cross_bf16_i8_w", "bf16", "i8", 1, 16, 1, 64, 64, 16448, 512, 16385, weights=True, causal=False),
+        # ---- evict
+        # 60 % of an image's 576 tokens and its CLS token, the smallest call
+        _evict("evict_577_i8", "i8", 1, 16, 64, 64, 640, 577, 347, 1, 0),
+        # sequences of up to 16000 tokens down to 4096 each, with 4 first and 256 last ones that stay
+        _evict("evict_16000_b8_e4m3", "e4m3", 8, 8, 128, 32, 16384, 16000, 4096, 4, 256),
+        # one long sequence, a quarter of it left
+        _evict("evict_131001_i8", "i8", 1, 8, 128, 128, 131072, 131001, 32768, 4, 1024),
+    ]
+
+
+def _cache(name, kind, code, batch, heads_kv, head_dim, block, capacity, longest):
+    return {"name": name, "kind": kind, "code": code, "batch": batch, "heads_kv": heads_kv, "head_dim": head_dim, "block": block,
+            "capacity": capacity, "longest": longest}
+
+
+def _append(name, dtype, code, batch, heads_kv, head_dim, block, capacity, tokens, longest):
+    return {**_cache(name, "append", code, batch, heads_kv, head_dim, block, capacity, longest), "dtype": dtype, "tokens": tokens}
+
+
+def _attend(name, dtype, code, batch, heads_kv, group, head_dim, block, capacity, tokens, longest, weights=False, causal=True):
+    return {**_cache(name, "attend", code, batch, heads_kv, head_dim, block, capacity, longest), "dtype": dtype, "group": group,
+            "tokens": tokens, "weights": weights, "causal": causal}
+
+
+def _evict(name, code, batch, heads_kv, head_dim, block, capacity, longest, keep, n_global, n_recent):
+    return {**_cache(name, "evict", code, batch, heads_kv, head_dim, block, capacity, longest), "keep": keep, "n_global": n_global,
+            "n_recent": n_recent}
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    while True:
+        case = _draw_any(rng)
+        del case["name"]
+        w = work(case)
+        held = case["batch"] * case["heads_kv"] * case["capacity"]
+        rows = held * case["group"] * case["tokens"] if case["kind"] == "attend" else 0
+        # no more than the listed ones cost: values of the cache, and the plain form's logits
+        if held * case["head_dim"] <= 1.4e8 and rows <= 1.1e9 and w["flops"] <= 2.8e11:
+            return case
+
+
+def _draw_any(rng):
+    kind = rng.choices(("append", "attend", "evict"), (2, 5, 2))[0]
+    code, dtype = rng.choice(("i8", "e4m3")), rng.choice(("f32", "bf16", "bf16", "bf16"))
+    batch, heads_kv = rng.choice((1, 1, 2, 3, 4, 8, 16, 32)), rng.choice((1, 2, 4, 8, 8, 16))
+    head_dim, block = rng.choice((64, 128, 128, 256)), rng.choice((16, 32, 64, 128))
+    longest = _log_int(rng, 1, 4500 if kind == "append" else 131072)
+    capacity = -(-longest // block) * block + block * rng.choice((0, 0, 1, 3))
+    if kind == "append":
+        return _append("", dtype, code, batch, heads_kv, head_dim, block, capacity, min(longest, rng.choice((1, _log_int(rng, 1, 4096)))), longest)
+    if kind == "attend":
+        tokens = min(longest, rng.choice((1, 1, _log_int(rng, 2, 16), _log_int(rng, 2, 4096))))
+        return _attend("", dtype, code, batch, heads_kv, rng.choice((1, 1, 2, 4, 7, 8)), head_dim, block, capacity, tokens, longest,
+                       weights=rng.random() < 0.5, causal=rng.random() < 0.8)
+    keep = max(1, int(longest * rng.uniform(0.1, 0.9)))
+    n_global = min(keep, rng.choice((0, 1, 4, 5)))
+    return _evict("", code, batch, heads_kv, head_dim, block, capacity, longest, keep, n_global, min(keep - n_global, rng.choice((0, 0, keep // 4))))
+
+
+# ---- inputs
+
+
+def _lengths(case):
+    """Tokens held by each sequence: the first one `longest`, in larger batches one slot empty, the others spread below."""
+    n, B = case["longest"], case["batch"]
+    return [n if b == 0 else 0 if b == 1 and B >= 4 else 1 + int((n - 1) * (b * 0.6180339887 % 1)) for b in range(B)]
+
+
+def _counts(case):
+    return [min(case["tokens"], n) for n in _lengths(case)]
+
+
+def _heads(gen, shape, dim):
+    """Keys or values as projections give them: channels of different size."""
+    gain = torch.exp(0.5 * torch.randn((shape[1], 1, dim), generator=gen, device="cuda"))
+    return torch.randn((*shape, dim), generator=gen, device="cuda").mul_(gain)
+
+
+def _fit(most, code):
+    """The smallest power of two s with most <= limit * s (2^-100 where there is nothing to hold)."""
+    m, e = torch.frexp(most)
+    top, shift = {"i8": (127 / 128, 7), "e4m3": (448 / 512, 9)}[code]
+    e = torch.where(m > top, e - shift + 1, e - shift)
+    return torch.ldexp(torch.ones_like(most), torch.where(most > 0, e, -100).clamp(min=-100))
+
+
+def _codes(y, code):
+    return (y.round() if code == "i8" else y).to(CODES[code][0])
+
+
+def _held(codes, scale):
+    """The values [B,H,N,D] that codes stand for, in fp32."""
+    B, H, N, D = codes.shape
+    return (codes.float().view(B, H, scale.shape[2], -1, D) * scale[..., None, None]).view(B, H, N, D)
+
+
+def _filled(case, gen):
+    """Codes and scales of a full cache's keys or values (also behind the sequences' ends: what was there before)."""
+    B, H, D, N, block = (case[k] for k in ("batch", "heads_kv", "head_dim", "capacity", "block"))
+    x = _heads(gen, (B, H, N), D).view(B, H, N // block, block, D)
+    scale = _fit(x.abs().amax((3, 4)), case["code"])
+    return _codes(x / scale[..., None, None], case["code"]).view(B, H, N, D), scale
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    B, H, D, N = (case[k] for k in ("batch", "heads_kv", "head_dim", "capacity"))
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    s = {"case": case, "lengths": ints(_lengths(case))}
+    s["k"], s["k_scale"] = _filled(case, gen)
+    s["v"], s["v_scale"] = _filled(case, gen)
+    if case["kind"] != "evict":
+        dtype, T = torch.float32 if case["dtype"] == "f32" else torch.bfloat16, case["tokens"]
+        s["counts"] = ints(_counts(case))
+    if case["kind"] == "append":
+        s["start"] = s["lengths"] - s["counts"]
+        # views of one projection's output [B, T, 2, H, D]
+        x = torch.stack([_heads(gen, (B, H, T), D) * 1.5 for _ in range(2)], 2).permute(0, 3, 2, 1, 4).contiguous().to(dtype)
+        s["new_k"], s["new_v"] = (x[:, :, i].transpose(1, 2) for i in range(2))
+    elif case["kind"] == "attend":
+        s["scale"] = 1.5 / D
+        s["q"] = _heads(gen, (B, H * case["group"], T), D).transpose(1, 2).contiguous().to(dtype).transpose(1, 2)
+        if case["weights"]:
+            w = _weights(case, gen, s["lengths"])                              # of some steps like this one
+            s["weights"] = w * (4 * T * case["group"] / w.sum(2, keepdim=True).clamp(min=1e-30))
+    else:
+        s["weights"] = _weights(case, gen, s["lengths"])
+        n = -(-case["keep"] // case["block"]) * case["block"]
+        for k in ("k", "v"):
+            s["to_" + k] = torch.zeros((B, H, n, D), dtype=s["k"].dtype, device="cuda")
+            s["to_%s_scale" % k] = torch.ones((B, H, n // case["block"]), device="cuda")
+    return s
+
+
+def _weights(case, gen, lengths):
+    """Added-up weights of the held tokens: a few large, many next to nothing, many of those equal; none behind the end."""
+    w = torch.exp(3 * torch.randn((case["batch"], case["heads_kv"], case["capacity"]), generator=gen, device="cuda") - 4)
+    w = torch.where(w < 0.01, (w * 2000).round() / 2000, w)
+    return w * (torch.arange(case["capacity"], device="cuda") < lengths[:, None, None])
+
+
+# ---- one pass
+
+
+def run(s):
+    if own:
+        return _run_own(s)
+    return {"append": _plain_append, "attend": _plain_attend, "evict": _plain_evict}[s["case"]["kind"]](s)
+
+
+def _run_own(s):
+    from paper_2601_12150_amd import binding as nb
+    case = s["case"]
+    cache = nb.kv_cache(s["k"], s["v"], s["k_scale"], s["v_scale"])
+    if case["kind"] == "append":
+        nb.kv_cache_append(cache, s["new_k"], s["new_v"], s["start"], counts=s["counts"])
+        return nb.kv_cache_read(cache, s["lengths"])
+    if case["kind"] == "attend":
+        return nb.kv_cache_attn(cache, s["q"], s["lengths"], counts=s["counts"], scale=s["scale"], causal=case["causal"], want_lse=True,
+                                weights=s.get("weights"))
+    to = nb.kv_cache(s["to_k"], s["to_v"], s["to_k_scale"], s["to_v_scale"])
+    kept, weights, lengths = nb.kv_cache_evict(cache, to, s["weights"], s["lengths"], case["keep"], n_global=case["n_global"],
+                                               n_recent=case["n_recent"])
+    return (kept, weights, lengths, *nb.kv_cache_read(to, lengths))
+
+
+def _plain_read(k, k_scale, v, v_scale, lengths):
+    there = (torch.arange(k.shape[2], device=k.device) < lengths[:, None])[:, None, :, None]
+    return tuple(torch.where(there, _held(c, sc), 0).to(torch.bfloat16) for c, sc in ((k, k_scale), (v, v_scale)))
+
+
+def _plain_append(s):
+    case = s["case"]
+    N, block, T = case["capacity"], case["block"], case["tokens"]
+    start, end = (x[:, None] for x in (s["start"], s["start"] + s["counts"]))
+    at = torch.arange(N, device="cuda")
+    new = (at >= start) & (at < end)                                           # [B,N]
+    first = at[::block]
+    touched = (first < end) & (first + block > start)                          # [B,N/block]
+    live = touched & (first < start)
+    source = (at - start).clamp(0, T - 1)[:, None, :, None]
+    for codes, scale, x in ((s["k"], s["k_scale"], s["new_k"]), (s["v"], s["v_scale"], s["new_v"])):
+        B, H, _, D = codes.shape
+        x = torch.where(new[:, None, :, None], x.float().gather(2, source.expand(B, H, N, D)), 0)
+        need = _fit(x.abs().view(B, H, N // block, block * D).amax(3), case["code"])
+        to = torch.where(live[:, None], torch.maximum(scale, need), need)
+        to = torch.where(touched[:, None], to, scale)
+        y = torch.where(new[:, None, :, None], x, _held(codes, scale)).view(B, H, N // block, block, D) / to[..., None, None]
+        codes.copy_(_codes(y, case["code"]).view(B, H, N, D))
+        scale.copy_(to)
+    return _plain_read(s["k"], s["k_scale"], s["v"], s["v_scale"], s["lengths"])
+
+
+def _plain_attend(s):
+    case = s["case"]
+    B, Hkv, N, D = s["k"].shape
+    T, G = case["tokens"], case["group"]
+    k, v = _held(s["k"], s["k_scale"]), _held(s["v"], s["v_scale"])
+    z = torch.matmul(s["q"].float().reshape(B, Hkv, G * T, D), k.transpose(2, 3).contiguous()).mul_(s["scale"]).view(B, Hkv, G, T, N)
+    t, n = torch.arange(T, device="cuda"), torch.arange(N, device="cuda")
+    lengths, counts = (s[k][:, None, None] for k in ("lengths", "counts"))
+    seen = (n < lengths) & (t[:, None] < counts)
+    if case["causal"]:
+        seen = seen & (n <= lengths - counts + t[:, None])
+    z.masked_fill_(~seen[:, None, None], -math.inf)
+    most = z.amax(4, keepdim=True)
+    most = torch.where(most == -math.inf, 0, most)
+    p = z.sub_(most).exp_()
+    total = p.sum(4, keepdim=True)
+    p.div_(torch.where(total == 0, 1, total))
+    out = torch.matmul(p.view(B, Hkv, G * T, N), v).view(B, Hkv * G, T, D).to(s["q"].dtype)
+    result = out, (most + total.log()).view(B, Hkv * G, T)
+    return (*result, s["weights"] + p.sum((2, 3))) if case["weights"] else result
+
+
+def _plain_evict(s):
+    case = s["case"]
+    keep, block = case["keep"], case["block"]
+    B, H, N, D = s["k"].shape
+    n, lengths = torch.arange(N, device="cuda"), s["lengths"][:, None]
+    stay = (n < case["n_global"]) | (n >= lengths - case["n_recent"])
+    rank = torch.where(stay[:, None], math.inf, s["weights"])
+    rank = torch.where((n < lengths)[:, None], rank, -math.inf)
+    best = rank.sort(dim=2, descending=True, stable=True).indices[:, :, :keep]
+    kept = torch.where(best < lengths[:, :, None], best, N).sort(dim=2).values  # the places behind a short sequence last
+    there = kept < N
+    left = torch.minimum(s["lengths"], torch.tensor(keep, dtype=torch.int32, device="cuda"))
+    weights = torch.where(there, s["weights"].gather(2, kept.clamp(max=N - 1)), 0)
+    M = s["to_k"].shape[2]
+    source = torch.nn.functional.pad(kept, (0, M - keep), value=N)
+    for to, to_scale, codes, scale in ((s["to_k"], s["to_k_scale"], s["k"], s["k_scale"]), (s["to_v"], s["to_v_scale"], s["v"], s["v_scale"])):
+        x = _held(codes, scale).gather(2, source.clamp(max=N - 1)[..., None].expand(B, H, M, D))
+        x = torch.where((source < N)[..., None], x, 0).view(B, H, M // block, block, D)
+        new = _fit(x.abs().amax((3, 4)), case["code"])
+        to.copy_(_codes(x / new[..., None, None], case["code"]).view(B, H, M, D))
+        to_scale.copy_(new)
+    values = _plain_read(s["to_k"], s["to_k_scale"], s["to_v"], s["to_v_scale"], left)
+    return (torch.where(there, kept, -1).int(), torch.nn.functional.pad(weights, (0, M - keep)), left, *values)
+
+
+# ---- what a pass cannot do without
+
+
+def work(case):
+    H, D, block = case["heads_kv"], case["head_dim"], case["block"]
+    lengths = _lengths(case)
+    token = 2 * D + 8 / block                                                  # a held token of one head, with its share of the scales
+    if case["kind"] == "append":
+        new, blocks = sum(_counts(case)), sum((n - c) % block for n, c in zip(lengths, _counts(case)))
+        es = 4 if case["dtype"] == "f32" else 2
+        back = sum(lengths) * (token + 4 * D)                                  # what is held, read back in bf16
+        zeros = (case["batch"] * case["capacity"] - sum(lengths)) * 4 * D
+        return {"bytes": H * (new * (2 * D * es + token) + blocks * token + back + zeros), "flops": 4.0 * H * new * D}
+    if case["kind"] == "attend":
+        es, rows = 4 if case["dtype"] == "f32" else 2, case["batch"] * H * case["group"] * case["tokens"]
+        pairs = sum(c * n - (c * (c - 1) // 2 if case["causal"] else 0) for c, n in zip(_counts(case), lengths))
+        w = 8 * case["batch"] * case["capacity"] * H if case["weights"] else 0
+        return {"bytes": H * sum(lengths) * token + rows * (2 * D * es + 4) + w, "flops": 4.0 * D * H * case["group"] * pairs}
+    kept, M = [min(case["keep"], n) for n in lengths], -(-case["keep"] // block) * block
+    ranked = 4 * sum(lengths)
+    back = sum(kept) * token + case["batch"] * M * 4 * D
+    return {"bytes": H * (ranked + 2 * sum(kept) * token + 4 * case["batch"] * (M + case["keep"]) + back), "flops": 2.0 * H * sum(kept) * D}
+
+
+# ---- the same in 64 bits, from the definitions
+
+
+def _exact_quantised(x, code):
+    """Codes (as numbers) and scales of x [..., block, D], in 64 bits."""
+    most = x.abs().amax((-2, -1), keepdim=True)
+    limit = CODES[code][1]
+    e = torch.floor(torch.log2(torch.clamp(most, min=1e-300) / limit))
+    e = torch.where(most > limit * torch.exp2(e), e + 1, e)
+    e = torch.where(most > limit * torch.exp2(e), e + 1, e)
+    e = torch.where(most <= limit * torch.exp2(e - 1), e - 1, e).clamp(min=-100)
+    return _exact_rounded(x / torch.exp2(e), code), torch.exp2(e)
+
+
+def _exact_rounded(y, code):
+    if code == "i8":
+        return torch.round(y)
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)     # 3 bits behind the first one, 2^-9 at least
+    return torch.round(y / step) * step
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    B, H, N, D = s["k"].shape
+    block, code = case["block"], case["code"]
+    lengths = _lengths(case)
+    blocks = lambda x: x.reshape(B, H, -1, block, D)  # noqa: E731
+    k, v = (s[n].double() for n in ("k", "v"))
+    ks, vs = (s[n].double()[..., None, None] for n in ("k_scale", "v_scale"))
+    if case["kind"] == "append":
+        got = []
+        for codes, scale, x in ((k, ks, s["new_k"].double()), (v, vs, s["new_v"].double())):
+            value = (blocks(codes) * scale).view(B, H, N, D)
+            for b in range(B):
+                at, count = lengths[b] - _counts(case)[b], _counts(case)[b]
+                if not count:
+                    continue
+                lo, hi = at // block, (at + count - 1) // block + 1
+                old = value[b, :, lo * block:at].clone()
+                fresh = torch.zeros((H, (hi - lo) * block, D), dtype=torch.float64, device="cuda")
+                fresh[:, at - lo * block:at - lo * block + count] = x[b, :, :count]
+                _, to = _exact_quantised(fresh.view(H, hi - lo, block, D), code)
+                if at > lo * block:
+                    to[:, 0] = torch.maximum(to[:, 0], scale[b, :, lo])
+                    fresh[:, :at - lo * block] = old
+                value[b, :, lo * block:hi * block] = (_exact_rounded(fresh.view(H, hi - lo, block, D) / to, code) * to).view(H, -1, D)
+            for b in range(B):
+                value[b, :, lengths[b]:] = 0
+            got.append(value)
+        return tuple(got)
+    if case["kind"] == "attend":
+        G, T = case["group"], case["tokens"]
+        out = torch.zeros((B, H * G, T, D), dtype=torch.float64, device="cuda")
+        lse = torch.full((B, H * G, T), -math.inf, dtype=torch.float64, device="cuda")
+        weights = s["weights"].double() if case["weights"] else None
+        k, v = (blocks(k) * ks).view(B, H, N, D), (blocks(v) * vs).view(B, H, N, D)
+        q = s["q"].double()
+        for b in range(B):
+            n, c = lengths[b], _counts(case)[b]
+            if not n:
+                continue
+            for h in range(H):
+                z = s["scale"] * (q[b, h * G:(h + 1) * G, :c].reshape(G * c, D) @ k[b, h, :n].T.contiguous()).view(G, c, n)
+                if case["causal"]:
+                    z += torch.full((c, n), -math.inf, dtype=torch.float64, device="cuda").triu(n - c + 1)
+                lse[b, h * G:(h + 1) * G, :c] = z.logsumexp(2)
+                p = z.softmax(2)
+                out[b, h * G:(h + 1) * G, :c] = (p.view(G * c, n) @ v[b, h, :n]).view(G, c, D)
+                if weights is not None:
+                    weights[b, h, :n] += p.sum((0, 1))
+        return (out, lse, weights) if case["weights"] else (out, lse)
+    keep, M = case["keep"], s["to_k"].shape[2]
+    kept = torch.full((B, H, keep), -1, dtype=torch.int32, device="cuda")
+    weights = torch.zeros((B, H, M), dtype=torch.float64, device="cuda")
+    values = [torch.zeros((B, H, M, D), dtype=torch.float64, device="cuda") for _ in range(2)]
+    for b in range(B):
+        n = lengths[b]
+        first, last = min(case["n_global"], n), max(n - case["n_recent"], min(case["n_global"], n))
+        for h in range(H):
+            at = torch.arange(n, device="cuda")
+            if n > keep:
+                ranked = torch.sort(s["weights"][b, h, first:last].double(), descending=True, stable=True).indices + first
+                at = torch.cat([at[:first], ranked[:keep - first - (n - last)], at[last:]]).sort().values
+            m = len(at)
+            kept[b, h, :m] = at.int()
+            weights[b, h, :m] = s["weights"][b, h, at].double()
+            for value, codes, scale in ((values[0], k, ks), (values[1], v, vs)):
+                value[b, h, :m] = codes[b, h, at] * scale[b, h, at // block, 0]
+    read = []
+    for value in values:
+        q, scale = _exact_quantised(blocks(value), code)
+        read.append((q * scale).view(B, H, M, D))
+    return (kept, weights, torch.tensor([min(n, keep) for n in lengths], dtype=torch.int32, device="cuda"), *read)
