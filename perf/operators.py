@@ -98,7 +98,7 @@ def _draw_any(rng):
     kind = rng.choices(("append", "attend", "evict"), (2, 5, 2))[0]
     code, dtype = rng.choice(("i8", "e4m3")), rng.choice(("f32", "bf16", "bf16", "bf16"))
     batch, heads_kv = rng.choice((1, 1, 2, 3, 4, 8, 16, 32)), rng.choice((1, 2, 4, 8, 8, 16))
-    head_dim, block = rng.choice((64, 128, 128, 256)), rng.choice((16, 32, 64, 128))
+    head_dim, block = rng.choice((64, 128, 128, 256)), rng.choice((32, 64, 128))
     longest = _log_int(rng, 1, 4500 if kind == "append" else 131072)
     capacity = -(-longest // block) * block + block * rng.choice((0, 0, 1, 3))
     if kind == "append":
