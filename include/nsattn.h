@@ -6,7 +6,8 @@
  * The operations follow the paper's Methodology section:
  *   "Memory-Efficiency Optimization"  -> ns_attn_forward, ns_attn_forward_scores
  *   "Time-Efficiency Optimization"    -> cls_scores, cls_scores_from_logits, topk_filter
- * and vit_block_forward wraps the attention in a pre-LayerNorm transformer block.
+ * and vit_block_forward wraps the attention in a pre-LayerNorm transformer block.  The kv_cache_* functions hold the
+ * keys and values of tokens in 8 bits for a model that reads them call by call, and rank and evict those by weight.
  *
  * Conventions that hold for every entry point
  *   - Token order: tokens 0..n_global-1 are global (CLS), token n_global + r*grid_w + c
@@ -306,6 +307,112 @@ size_t vit_embed_workspace_bytes(int32_t batch, int32_t channels, int32_t grid_h
 ns_status vit_embed(int32_t batch, int32_t channels, int32_t grid_h, int32_t grid_w, int32_t patch, int32_t dim,
                     const void *pixels, const void *w_patch, const float *b_patch, const void *cls_token,
                     const void *pos_embed, void *x_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A cache of keys and values in 8 bits, for a model that reads the tokens a backbone kept and holds them, and its own,
+ * from call to call.  For every sequence b and key/value head h it has room for `capacity` tokens of head_dim values:
+ *     value[b,h,n,d] = code[b,h,n,d] * scale[b,h,n / block]
+ * with one scale for each block of tokens, keys and values apart.  The struct only describes the caller's memory; how many
+ * tokens a sequence holds is not part of it (the layers of a model share those counts), every call is told.
+ *
+ * Codes are int8 (-127..127) or OCP e4m3.  The scales that the library writes are powers of two: the smallest s of at least
+ * 2^-100 with max |x| <= 127 s (e4m3: 448 s) over the block's tokens.  So x / s is exact, codes are the nearest ones to x / s
+ * (ties to even), and every value has at most 8 significant bits (exact in bf16).  Scales that the caller writes may be any
+ * finite floats above 0.  A NaN scale stands for a block that was given a NaN or an infinity: all its tokens' values are NaN.
+ *
+ * Tokens are in order: position n is token n of the sequence, 0 <= n < its length.  What lies behind a sequence's length is
+ * never used, whatever it is.
+ */
+typedef enum { NS_CODE_I8 = 0, NS_CODE_E4M3 = 1 } ns_kv_code;
+
+typedef struct ns_kv_cache {
+  int32_t batch;     /* B >= 1 sequences; NS_ERR_UNSUPPORTED above 65535                  */
+  int32_t heads_kv;  /* key/value heads; at most 1024                                    */
+  int32_t head_dim;  /* D: 64, 128 or 256                                                */
+  int32_t capacity;  /* tokens there is room for: a multiple of block, at most 2^30      */
+  int32_t block;     /* tokens that share a scale: 32, 64 or 128                         */
+  int32_t code;      /* ns_kv_code                                                       */
+  int64_t stride_b, stride_h, stride_t; /* strides of k and v in bytes: multiples of 16, not negative, stride_t >= D
+                        (calls that only read take 0 too: sequences that share what they hold)   */
+  void *k, *v;                /* codes, 16-byte aligned; the D codes of a token are contiguous   */
+  float *k_scale, *v_scale;   /* [B, heads_kv, capacity / block]                         */
+} ns_kv_cache;
+
+/*
+ * New keys and values enter the cache: token t < counts[b] of sequence b goes to position start[b] + t.
+ *   k, v    in  [B, heads_kv, tokens, D] of type dtype (ns_dtype) with the given element strides (both the same; rows
+ *               16-byte aligned, D contiguous)
+ *   start   in  device [B] int32: the tokens held before; below 0 is taken as 0
+ *   counts  in, nullable  device [B] int32: new tokens of each sequence (padded batch), taken into 0..tokens; NULL: tokens
+ * Tokens that the capacity has no room for are dropped.  A block that the new tokens enter from its first position on gets
+ * the scale they need.  One that holds tokens before start[b] keeps its scale where that suffices for the new tokens (their
+ * magnitudes are at most 127 or 448 times the scale); else it gets the one they need, to which the codes before are rounded again.  Other blocks and positions are left as they are.
+ * Two calls that enter the same tokens leave the same cache.
+ */
+ns_status kv_cache_append(const ns_kv_cache *cache, int32_t tokens, int32_t dtype, const void *k, const void *v,
+                          int64_t stride_b, int64_t stride_h, int64_t stride_t, const int32_t *start,
+                          const int32_t *counts, void *stream);
+
+/*
+ * Values of the positions first .. first + tokens - 1, which must lie within the capacity, in dtype (ns_dtype; bf16: the
+ * nearest, exact for the library's own scales).
+ *   lengths      in   device [B] int32: tokens held; positions from there on read as zeros
+ *   k_out, v_out out  contiguous [B, heads_kv, tokens, D], 16-byte aligned
+ */
+ns_status kv_cache_read(const ns_kv_cache *cache, const int32_t *lengths, int32_t first, int32_t tokens, int32_t dtype,
+                        void *k_out, void *v_out, void *stream);
+
+/*
+ * Attention of `tokens` queries per sequence and head to what the cache holds.  Query head hq reads key/value head
+ * hq / (heads / heads_kv).
+ *   q        in   [B, heads, tokens, D] by the descriptor's q strides;  out  likewise, with its own strides
+ *   lengths  in   device [B] int32: tokens held, those of the queries included; taken into 0..capacity
+ *   counts   in, nullable  device [B] int32: queries of each sequence (padded batch), taken into 0..tokens; NULL: tokens
+ *   causal   non-zero: query t < counts[b] stands at position lengths[b] - counts[b] + t and sees the positions up to its
+ *            own.  0: every query sees all lengths[b] positions.
+ *   lse      out, nullable  [B, heads, tokens] fp32: log of the sum of exp(logits)
+ *   weights_in  in, nullable, weights_out out, nullable  [B, heads_kv, capacity] fp32: weights_out = weights_in (NULL: 0)
+ *            plus, for every position, the softmax weights that all queries of the heads that read it give it.  The two may
+ *            be the same memory; positions from lengths[b] on are then left as they are.
+ * A query that sees nothing (an empty sequence, t >= counts[b]) gets zeros, lse -inf, and gives no weight.
+ * Logits, softmax and sums are fp32.
+ */
+typedef struct ns_kv_attn_desc {
+  int32_t heads;     /* query heads: a multiple of heads_kv, at most 1024; heads * tokens at most 2^24 */
+  int32_t tokens;    /* queries per sequence and head                                    */
+  int32_t dtype;     /* ns_dtype of q and out                                            */
+  int32_t causal;
+  float scale;       /* logit multiplier, normally 1/sqrt(D); finite                     */
+  int64_t q_stride_b, q_stride_h, q_stride_t;       /* element strides, rows 16-byte aligned */
+  int64_t out_stride_b, out_stride_h, out_stride_t;
+} ns_kv_attn_desc;
+
+/* Bytes of workspace (256-byte aligned) a call needs; want_weights: with weights_out.  0 where the call is refused, and
+ * where it needs none. */
+size_t kv_cache_attn_workspace_bytes(const ns_kv_cache *cache, const ns_kv_attn_desc *desc, int32_t want_weights);
+ns_status kv_cache_attn(const ns_kv_cache *cache, const ns_kv_attn_desc *desc, const void *q, const int32_t *lengths,
+                        const int32_t *counts, void *out, float *lse, const float *weights_in, float *weights_out,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Eviction by added-up weight: of every sequence and key/value head, keep tokens stay and move together, in order, into
+ * another cache (same batch, heads_kv, head_dim, block and code; room for `keep` tokens at least; memory of its own).
+ * A sequence of at most keep tokens stays whole.  Of a longer one stay: the first n_global, the last n_recent
+ * (n_global + n_recent <= keep), and of the others those with the largest weights; equal ones (-0 == +0) rank by lower
+ * position first, NaN above everything.  Every head has its own choice.
+ *   weights     in   [B, heads_kv, from->capacity] fp32, as kv_cache_attn adds them up
+ *   lengths     in   device [B] int32; taken into 0..from->capacity
+ *   kept_idx    out  [B, heads_kv, keep] int32: the positions they had, ascending; -1 behind them
+ *   weights_out out  [B, heads_kv, to->capacity] fp32: their weights, 0 behind them
+ *   lengths_out out  [B] int32: min(lengths[b], keep); memory of its own
+ * A block of the new cache gets the scale that its tokens need; their codes are rounded to it.  Codes behind the last token
+ * of its block become 0, further blocks are left as they are.
+ *   workspace   kv_cache_evict_workspace_bytes(...) bytes, 256-byte aligned (0 bytes: NULL is accepted)
+ */
+size_t kv_cache_evict_workspace_bytes(const ns_kv_cache *from, int32_t keep);
+ns_status kv_cache_evict(const ns_kv_cache *from, const ns_kv_cache *to, const float *weights, const int32_t *lengths,
+                         int32_t keep, int32_t n_global, int32_t n_recent, int32_t *kept_idx, float *weights_out,
+                         int32_t *lengths_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Measurement aid for benchmarks (not part of the method): enqueues `reps` launches of the

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -19,12 +19,15 @@ LIB_PATH = os.path.join(_HERE, "libnsattn.so")
 
 NS_OK, NS_ERR_INVALID_ARG, NS_ERR_UNSUPPORTED, NS_ERR_WORKSPACE, NS_ERR_HIP = range(5)
 NS_F32, NS_BF16 = 0, 1
+NS_CODE_I8, NS_CODE_E4M3 = 0, 1
 
 EXPORTS = ["ns_attn_workspace_bytes", "ns_attn_forward", "cls_scores_workspace_bytes", "cls_scores",
            "cls_scores_static_max_bytes", "cls_scores_static",
            "cls_scores_from_logits", "ns_attn_forward_scores", "topk_filter_workspace_bytes", "topk_filter", "topk_filter_global", "vit_forward_features",
            "vit_embed_workspace_bytes", "vit_embed", "vit_block_workspace_bytes", "vit_block_forward", "linear_forward", "vit_workspace_bytes", "vit_forward",
            "vit_stages_workspace_bytes", "vit_forward_stages",
+           "kv_cache_append", "kv_cache_read", "kv_cache_attn_workspace_bytes", "kv_cache_attn", "kv_cache_evict_workspace_bytes",
+           "kv_cache_evict",
            "ns_attn_patch_kernel_time", "ns_attn_patch_kernel_name", "ns_last_error",
            "ns_version"]
 
@@ -44,6 +47,17 @@ class ns_attn_desc(ctypes.Structure):
                 ("q_stride_t", ctypes.c_int64), ("out_stride_b", ctypes.c_int64),
                 ("out_stride_h", ctypes.c_int64), ("out_stride_t", ctypes.c_int64),
                 ("coords", ctypes.c_void_p)]
+
+
+class ns_kv_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "heads_kv", "head_dim", "capacity", "block", "code")] + \
+               [(n, ctypes.c_int64) for n in ("stride_b", "stride_h", "stride_t")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class ns_kv_attn_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "tokens", "dtype", "causal")] + [("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_stride_b", "q_stride_h", "q_stride_t", "out_stride_b", "out_stride_h", "out_stride_t")]
 
 
 class ns_vit_block_desc(ctypes.Structure):
@@ -122,6 +136,15 @@ def _load() -> ctypes.CDLL:
                                        ctypes.POINTER(ns_vit_block_weights), vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.vit_forward_features.argtypes = [ctypes.POINTER(ns_vit_desc), ctypes.POINTER(ns_vit_block_weights), vp, vp,
                                          vp, i32, ctypes.POINTER(i32), ctypes.POINTER(vp), vp, sz, vp]
+    cp, i64 = ctypes.POINTER(ns_kv_cache), ctypes.c_int64
+    kp = ctypes.POINTER(ns_kv_attn_desc)
+    for f, res, args in ((lib.kv_cache_append, ctypes.c_int, [cp, i32, i32, vp, vp, i64, i64, i64, vp, vp, vp]),
+                         (lib.kv_cache_read, ctypes.c_int, [cp, vp, i32, i32, i32, vp, vp, vp]),
+                         (lib.kv_cache_attn_workspace_bytes, sz, [cp, kp, i32]),
+                         (lib.kv_cache_attn, ctypes.c_int, [cp, kp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+                         (lib.kv_cache_evict_workspace_bytes, sz, [cp, i32]),
+                         (lib.kv_cache_evict, ctypes.c_int, [cp, cp, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp])):
+        f.restype, f.argtypes = res, args
     lib.ns_last_error.restype = ctypes.c_char_p
     lib.ns_version.restype = ctypes.c_char_p
     return lib
@@ -360,3 +383,64 @@ def vit_forward_stages(x, layer_weights, grid_h, grid_w, block, heads, stage_aft
     _check(lib.vit_forward_stages(ctypes.byref(d), ns, aft, kp, warr, _ptr(x), _ptr(out), _ptr(kept), _ptr(ws),
                                   ws.numel(), _stream(stream)))
     return out, kept
+
+
+class kv_cache(NamedTuple):
+    """Keys and values in 8 bits (the ns_kv_cache of the C ABI): k, v [B,H,capacity,D] int8 or float8_e4m3fn codes with equal
+    strides, k_scale, v_scale [B,H,capacity/block] float32; value = code * scale."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def kv_cache_empty(batch, heads, capacity, head_dim, block=64, dtype=torch.int8, device="cuda") -> kv_cache:
+    """A contiguous cache with room for `capacity` tokens (a multiple of `block`), codes 0 and scales 1."""
+    if block < 1 or capacity % block:
+        raise ValueError("capacity must be a multiple of block")
+    codes = [torch.zeros((batch, heads, capacity, head_dim), dtype=torch.uint8, device=device).view(dtype) for _ in range(2)]
+    scales = [torch.ones((batch, heads, capacity // block), dtype=torch.float32, device=device) for _ in range(2)]
+    return kv_cache(*codes, *scales)
+
+
+def _on(stream, f, *args):
+    """f(*args, None) with `stream` as the current stream: what the binding allocates then belongs to it."""
+    if stream is None:
+        return f(*args, None)
+    with torch.cuda.stream(stream):
+        return f(*args, None)
+
+
+def kv_cache_append(cache, k, v, start, counts=None, stream=None) -> None:
+    """New keys and values k, v [B,H,T,D] (float32 or bfloat16, equal strides) enter the cache at the positions from
+    start [B] int32; counts [B] int32: how many of the T are valid (padded batch)."""
+    _on(stream, _nsbind.kv_append, cache, k, v, start, counts)
+
+
+def kv_cache_read(cache, lengths, first=0, tokens=None, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
+    """Values of the positions first .. first + tokens - 1 (to the end when None): (k, v) [B,H,tokens,D] in dtype, zeros from
+    lengths [B] int32 on."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("only float32 and bfloat16 tensors are supported, got %s" % dtype)
+    return _on(stream, _nsbind.kv_read, cache, lengths, first, tokens, dtype == torch.bfloat16, k_out, v_out)
+
+
+def kv_cache_attn(cache, q, lengths, counts=None, scale=None, causal=True, out=None, want_lse=False, weights=None,
+                  weights_out=None, want_weights=False, workspace=None, stream=None):
+    """Attention of q [B,heads,T,D] (heads a multiple of the cache's) to the lengths [B] int32 tokens that the cache holds, those
+    of the queries included; counts [B] int32: how many of the T queries are valid.  causal: query t is at position
+    lengths - counts + t.
+
+    Returns out [B,heads,T,D]; with want_lse also the log-sum-exp [B,heads,T]; with want_weights, weights or weights_out
+    also the weights [B,H,capacity] that the tokens were given, added to `weights` where those are passed (weights_out=weights
+    adds in place)."""
+    return _on(stream, _nsbind.kv_attn, cache, q, lengths, counts, scale, causal, out, want_lse, weights, weights_out, want_weights,
+               workspace)
+
+
+def kv_cache_evict(cache, to, weights, lengths, keep, n_global=1, n_recent=0, workspace=None, stream=None):
+    """Of every sequence and head the n_global first, the n_recent last and the tokens with the largest weights
+    [B,H,capacity], `keep` in all, move together into the cache `to`.
+
+    Returns (kept_idx [B,H,keep] int32 ascending, -1 behind a shorter sequence, weights [B,H,to's capacity], lengths [B] int32)."""
+    return _on(stream, _nsbind.kv_evict, cache, to, weights, lengths, keep, n_global, n_recent, workspace)

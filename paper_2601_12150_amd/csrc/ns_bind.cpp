@@ -8,6 +8,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <cmath>
+#include <cstdint>
+#include <initializer_list>
 #include <vector>
 #include "../../include/nsattn.h"
 
@@ -411,6 +413,195 @@ PyObject *stack(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- the 8-bit key/value cache: (k, v, k_scale, v_scale)
+
+// Everything a call works on lies on the current device, whose stream it takes.
+void on_current_device(std::initializer_list<const at::Tensor *> ts) {
+  int64_t dev = -1;
+  for (const at::Tensor *t : ts) {
+    if (!t->defined()) continue;
+    if (!t->is_cuda()) value_error("all tensors must be on the GPU");
+    if (dev < 0) {
+      PyObject *o = PyObject_CallNoArgs(g_device);
+      if (!o) throw PyFail{};
+      dev = PyLong_AsLongLong(o);
+      Py_DECREF(o);
+    }
+    if (t->device().index() != dev) value_error("all tensors must be on the current device");
+  }
+}
+// The strides of [B,H,T,D]; that of a dimension of one, which torch leaves open, is what the C ABI takes.
+struct Strides {
+  int64_t b, h, t;
+  explicit Strides(const at::Tensor &x)
+      : b(x.size(0) > 1 ? x.stride(0) : 0), h(x.size(1) > 1 ? x.stride(1) : 0), t(x.size(2) > 1 ? x.stride(2) : x.size(3)) {
+    if (x.size(3) > 1 && x.stride(3) != 1) value_error("head_dim must be contiguous");
+  }
+  bool operator!=(const Strides &o) const { return b != o.b || h != o.h || t != o.t; }
+};
+struct Cache {
+  at::Tensor k, v, k_scale, v_scale;
+  ns_kv_cache c{};
+};
+Cache read_cache(PyObject *o) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) {
+    PyErr_SetString(PyExc_TypeError, "cache must be a kv_cache (k, v, k_scale, v_scale)");
+    throw PyFail{};
+  }
+  Cache r{tensor(PyTuple_GET_ITEM(o, 0), "k"), tensor(PyTuple_GET_ITEM(o, 1), "v"), tensor(PyTuple_GET_ITEM(o, 2), "k_scale"),
+          tensor(PyTuple_GET_ITEM(o, 3), "v_scale")};
+  const at::Tensor &k = r.k, &s = r.k_scale;
+  if (k.dim() != 4 || k.sizes() != r.v.sizes() || Strides(k) != Strides(r.v) || k.scalar_type() != r.v.scalar_type())
+    value_error("the cache's k and v must be [B,H,capacity,D] with the same strides and dtype");
+  const Strides st(k);
+  const bool i8 = k.scalar_type() == at::kChar;
+  if (!i8 && k.scalar_type() != at::kFloat8_e4m3fn) {
+    PyErr_Format(PyExc_TypeError, "a cache holds int8 or float8_e4m3fn codes, got torch.%s", c10::toString(k.scalar_type()));
+    throw PyFail{};
+  }
+  if (s.dim() != 3 || s.sizes() != r.v_scale.sizes() || s.size(0) != k.size(0) || s.size(1) != k.size(1) || s.size(2) < 1 || k.size(2) % s.size(2))
+    value_error("the cache's scales must be [B,H,capacity/block]");
+  for (const at::Tensor *t : {&r.k_scale, &r.v_scale})
+    if (t->scalar_type() != at::kFloat || !t->is_contiguous()) value_error("the cache's scales must be contiguous float32 tensors");
+  for (int64_t n : k.sizes())
+    if (n > INT32_MAX) value_error("the cache is too large");
+  ns_kv_cache &c = r.c;
+  c.batch = (int32_t)k.size(0); c.heads_kv = (int32_t)k.size(1); c.capacity = (int32_t)k.size(2); c.head_dim = (int32_t)k.size(3);
+  c.block = (int32_t)(k.size(2) / s.size(2));
+  c.code = i8 ? NS_CODE_I8 : NS_CODE_E4M3;
+  c.stride_b = st.b; c.stride_h = st.h; c.stride_t = st.t;
+  c.k = ptr(k); c.v = ptr(r.v);
+  c.k_scale = static_cast<float *>(ptr(r.k_scale)); c.v_scale = static_cast<float *>(ptr(r.v_scale));
+  return r;
+}
+const int32_t *counts_of(const at::Tensor &t, const Cache &c, const char *name) {
+  if (!t.defined()) return nullptr;
+  if (!i32_contiguous(t) || t.dim() != 1 || t.size(0) != c.c.batch) {
+    PyErr_Format(PyExc_ValueError, "%s must be a contiguous int32 tensor [B]", name);
+    throw PyFail{};
+  }
+  return static_cast<const int32_t *>(ptr(t));
+}
+int32_t int32(PyObject *o, const char *name) {
+  const int64_t v = integer(o);
+  if (v > INT32_MAX || v < INT32_MIN) {
+    PyErr_Format(PyExc_ValueError, "%s is out of range", name);
+    throw PyFail{};
+  }
+  return (int32_t)v;
+}
+float *weights_of(const at::Tensor &t, int64_t B, int64_t H, int64_t N, const char *name) {
+  if (!t.defined()) return nullptr;
+  if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.dim() != 3 || t.size(0) != B || t.size(1) != H || t.size(2) != N) {
+    PyErr_Format(PyExc_ValueError, "%s must be a contiguous float32 tensor [B,H,capacity]", name);
+    throw PyFail{};
+  }
+  return static_cast<float *>(ptr(t));
+}
+
+// kv_append(cache, k, v, start, counts, stream)
+PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject * {
+    const Cache c = read_cache(a[0]);
+    const at::Tensor &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &start = tensor(a[3], "start");
+    const at::Tensor counts = optional(a[4], "counts");
+    if (k.dim() != 4 || k.sizes() != v.sizes() || Strides(k) != Strides(v) || k.scalar_type() != v.scalar_type())
+      value_error("k and v must be [B,H,T,D] with the same strides and dtype");
+    if (k.size(0) != c.c.batch || k.size(1) != c.c.heads_kv || k.size(3) != c.c.head_dim) value_error("k and v must have the cache's B, H and D");
+    if (k.size(2) > INT32_MAX) value_error("too many tokens");
+    const Strides st(k);
+    const int dt = dtype_code(k);
+    const int32_t *sp = counts_of(start, c, "start"), *cp = counts_of(counts, c, "counts");
+    on_current_device({&c.k, &c.v, &c.k_scale, &c.v_scale, &k, &v, &start, &counts});
+    void *const s = stream_of(a[5]);
+    call([&] { return kv_cache_append(&c.c, (int32_t)k.size(2), dt, ptr(k), ptr(v), st.b, st.h, st.t, sp, cp, s); });
+    Py_RETURN_NONE;
+  });
+}
+
+// kv_read(cache, lengths, first, tokens, bf16, k_out, v_out, stream)
+PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject * {
+    const Cache c = read_cache(a[0]);
+    const at::Tensor &lengths = tensor(a[1], "lengths");
+    const int32_t first = int32(a[2], "first"), tokens = a[3] == Py_None ? c.c.capacity - first : int32(a[3], "tokens");
+    const int bf = PyObject_IsTrue(a[4]);
+    if (bf < 0) throw PyFail{};
+    const auto dt = bf ? at::kBFloat16 : at::kFloat;
+    const int32_t *lp = counts_of(lengths, c, "lengths");
+    at::Tensor out[2] = {optional(a[5], "k_out"), optional(a[6], "v_out")};
+    for (at::Tensor &t : out) {
+      if (!t.defined()) {
+        t = empty({c.c.batch, c.c.heads_kv, tokens > 0 ? tokens : 0, c.c.head_dim}, dt, c.k);
+      } else if (t.scalar_type() != dt || !t.is_contiguous() || t.sizes() != at::IntArrayRef({c.c.batch, c.c.heads_kv, tokens, c.c.head_dim})) {
+        value_error("k_out and v_out must be contiguous [B,H,tokens,D] tensors of the asked dtype");
+      }
+    }
+    on_current_device({&c.k, &c.v, &c.k_scale, &c.v_scale, &lengths, &out[0], &out[1]});
+    void *const s = stream_of(a[7]);
+    call([&] { return kv_cache_read(&c.c, lp, first, tokens, bf ? NS_BF16 : NS_F32, ptr(out[0]), ptr(out[1]), s); });
+    return tuple(out[0], out[1]);
+  });
+}
+
+// kv_attn(cache, q, lengths, counts, scale, causal, out, want_lse, weights, weights_out, want_weights, workspace, stream)
+PyObject *kv_attn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject * {
+    const Cache c = read_cache(a[0]);
+    const at::Tensor &q = tensor(a[1], "q"), &lengths = tensor(a[2], "lengths");
+    const at::Tensor counts = optional(a[3], "counts"), w_in = optional(a[8], "weights");
+    at::Tensor out = optional(a[6], "out"), w_out = optional(a[9], "weights_out"), lse;
+    if (q.dim() != 4 || q.size(0) != c.c.batch || q.size(3) != c.c.head_dim) value_error("q must be [B,heads,T,D] with the cache's B and D");
+    if (q.size(1) > INT32_MAX || q.size(2) > INT32_MAX) value_error("q is too large");
+    if (!out.defined()) out = empty(q.sizes(), q.scalar_type(), q);
+    if (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type()) value_error("out must have q's shape and dtype");
+    const Strides qs(q), os(out);
+    ns_kv_attn_desc d{};
+    d.heads = (int32_t)q.size(1); d.tokens = (int32_t)q.size(2);
+    d.dtype = dtype_code(q);
+    d.scale = scale_of(a[4], q.size(3));
+    const int causal = PyObject_IsTrue(a[5]), want_lse = PyObject_IsTrue(a[7]), want_w = PyObject_IsTrue(a[10]);
+    if (causal < 0 || want_lse < 0 || want_w < 0) throw PyFail{};
+    d.causal = causal;
+    d.q_stride_b = qs.b; d.q_stride_h = qs.h; d.q_stride_t = qs.t;
+    d.out_stride_b = os.b; d.out_stride_h = os.h; d.out_stride_t = os.t;
+    const int32_t *lp = counts_of(lengths, c, "lengths"), *cp = counts_of(counts, c, "counts");
+    const float *wi = weights_of(w_in, c.c.batch, c.c.heads_kv, c.c.capacity, "weights");
+    const bool weigh = want_w || w_in.defined() || w_out.defined();
+    if (weigh && !w_out.defined()) w_out = empty({c.c.batch, c.c.heads_kv, c.c.capacity}, at::kFloat, q);
+    float *const wo = weights_of(w_out, c.c.batch, c.c.heads_kv, c.c.capacity, "weights_out");
+    if (want_lse) lse = empty({q.size(0), q.size(1), q.size(2)}, at::kFloat, q);
+    const at::Tensor ws = workspace(a[11], kv_cache_attn_workspace_bytes(&c.c, &d, weigh), q);
+    on_current_device({&c.k, &c.v, &c.k_scale, &c.v_scale, &q, &lengths, &counts, &out, &w_in, &w_out, &ws});
+    void *const s = stream_of(a[12]);
+    call([&] { return kv_cache_attn(&c.c, &d, ptr(q), lp, cp, ptr(out), static_cast<float *>(ptr(lse)), wi, wo, ptr(ws), bytes_of(ws), s); });
+    if (want_lse) return weigh ? tuple(out, lse, w_out) : tuple(out, lse);
+    return weigh ? tuple(out, w_out) : wrap(out);
+  });
+}
+
+// kv_evict(cache, to, weights, lengths, keep, n_global, n_recent, workspace, stream)
+PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject * {
+    const Cache c = read_cache(a[0]), to = read_cache(a[1]);
+    const at::Tensor &w = tensor(a[2], "weights"), &lengths = tensor(a[3], "lengths");
+    const int32_t keep = int32(a[4], "keep"), G = int32(a[5], "n_global"), recent = int32(a[6], "n_recent");
+    const float *wp = weights_of(w, c.c.batch, c.c.heads_kv, c.c.capacity, "weights");
+    const int32_t *lp = counts_of(lengths, c, "lengths");
+    const int64_t B = c.c.batch, H = c.c.heads_kv;
+    const at::Tensor kept = empty({B, H, keep > 0 ? keep : 0}, at::kInt, c.k), left = empty({B}, at::kInt, c.k);
+    const at::Tensor w_out = empty({B, H, to.c.capacity}, at::kFloat, c.k);
+    const at::Tensor ws = workspace(a[7], kv_cache_evict_workspace_bytes(&c.c, keep), c.k);
+    on_current_device({&c.k, &c.v, &c.k_scale, &c.v_scale, &to.k, &to.v, &to.k_scale, &to.v_scale, &w, &lengths, &ws});
+    void *const s = stream_of(a[8]);
+    call([&] {
+      return kv_cache_evict(&c.c, &to.c, wp, lp, keep, G, recent, static_cast<int32_t *>(ptr(kept)), static_cast<float *>(ptr(w_out)),
+                            static_cast<int32_t *>(ptr(left)), ptr(ws), bytes_of(ws), s);
+    });
+    return tuple(kept, w_out, left);
+  });
+}
+
 // setup(error class, function giving the current device, function giving a device's current stream)
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 3, [&]() -> PyObject * {
@@ -426,7 +617,7 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 #define NS_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NS_FAST(attn), NS_FAST(scores), NS_FAST(topk), NS_FAST(embed), NS_FAST(block), NS_FAST(stack),
-                         NS_FAST(setup), {nullptr, nullptr, 0, nullptr}};
+                         NS_FAST(kv_append), NS_FAST(kv_read), NS_FAST(kv_attn), NS_FAST(kv_evict), NS_FAST(setup), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_nsbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
