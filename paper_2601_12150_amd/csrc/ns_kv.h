@@ -69,4 +69,54 @@ __device__ __forceinline__ float kv_scale_for(uint32_t most) {
 }
 __device__ __forceinline__ bool kv_is_nan(float s) { return !(s == s); }
 
+// ---- matrix products over codes
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+union Frag {                               // one lane's operand of a 16x16x32 or 32x32x16 product
+  f16x8 v;
+  uint32_t w[4];
+};
+
+// Codes as fp16, which holds every one of them exactly.  int8: the byte c + 128 (the code with its top bit turned) below the
+// byte 0x64 is 1024 + 128 + c in fp16, from which 1152 is taken: with the byte permutation one and a half instructions for two codes.
+// e4m3: a conversion of two.  The operand is one dword of codes prepared by kv_raw.
+template <int CODE> __device__ __forceinline__ uint32_t kv_raw(uint32_t w) { return CODE == NS_CODE_I8 ? w ^ 0x80808080u : w; }
+template <int CODE, int HALF> __device__ __forceinline__ uint32_t kv_f16x2(uint32_t raw) {      // the codes 2 HALF, 2 HALF + 1
+  if (CODE == NS_CODE_I8) {
+    const uint32_t u = __builtin_amdgcn_perm(0x64646464u, raw, HALF ? 0x07030602u : 0x05010400u);
+    const f16x2 c = __builtin_bit_cast(f16x2, u) - f16x2{(_Float16)1152, (_Float16)1152};
+    return __builtin_bit_cast(uint32_t, c);
+  }
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)raw, 1.f, HALF));
+}
+// eight consecutive codes
+template <int CODE> __device__ __forceinline__ Frag kv_frag(uint32_t lo, uint32_t hi) {
+  lo = kv_raw<CODE>(lo);
+  hi = kv_raw<CODE>(hi);
+  return Frag{.w = {kv_f16x2<CODE, 0>(lo), kv_f16x2<CODE, 1>(lo), kv_f16x2<CODE, 0>(hi), kv_f16x2<CODE, 1>(hi)}};
+}
+// The transpose: of eight tokens' dwords (four channels each) the four channels' fragments, tokens in order.
+template <int CODE> __device__ __forceinline__ void kv_frags_t(const uint32_t (&t)[8], Frag (&f)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    const uint32_t a = kv_raw<CODE>(t[2 * j]), b = kv_raw<CODE>(t[2 * j + 1]);
+    const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05010400u), hi = __builtin_amdgcn_perm(b, a, 0x07030602u);   // a0 b0 a1 b1, a2 b2 a3 b3
+    f[0].w[j] = kv_f16x2<CODE, 0>(lo);
+    f[1].w[j] = kv_f16x2<CODE, 1>(lo);
+    f[2].w[j] = kv_f16x2<CODE, 0>(hi);
+    f[3].w[j] = kv_f16x2<CODE, 1>(hi);
+  }
+}
+
+// ---- queries as fp16.  A row is scaled by a power of two that brings its largest magnitude to 2^14 .. 2^15: what lies 28 binades
+// below it keeps its 11 bits (bf16 has 8; fp32 is taken as the sum of two such numbers, 22 bits), what lies further below is off by at
+// most 2^-39 of the largest.
+__device__ __forceinline__ int kv_row_shift(uint32_t most) { return most >= kInfBits ? 0 : 141 - (int)(most >> 23); }   // q is taken times 2^this
+
+// positions that query t sees: 0 .. limit - 1
+__device__ __forceinline__ int kv_seen(const ns_kv_attn_desc &d, int t, int length, int count) {
+  return t >= count ? 0 : d.causal ? max(length - count + t + 1, 0) : length;
+}
+
 }  // namespace ns
