@@ -315,7 +315,7 @@ ns_status vit_embed(int32_t batch, int32_t channels, int32_t grid_h, int32_t gri
  * with one scale for each block of tokens, keys and values apart.  The struct only describes the caller's memory; how many
  * tokens a sequence holds is not part of it (the layers of a model share those counts), every call is told.
  *
- * Codes are int8 (-127..127) or OCP e4m3.  The scales that the library writes are powers of two: the smallest s of at least
+ * Codes are int8 (-127..127) or OCP e4m3 (no NaN).  The scales that the library writes are powers of two: the smallest s of at least
  * 2^-100 with max |x| <= 127 s (e4m3: 448 s) over the block's tokens.  So x / s is exact, codes are the nearest ones to x / s
  * (ties to even), and every value has at most 8 significant bits (exact in bf16).  Scales that the caller writes may be any
  * finite floats above 0.  A NaN scale stands for a block that was given a NaN or an infinity: all its tokens' values are NaN.
@@ -332,8 +332,8 @@ typedef struct ns_kv_cache {
   int32_t capacity;  /* tokens there is room for: a multiple of block, at most 2^30      */
   int32_t block;     /* tokens that share a scale: 32, 64 or 128                         */
   int32_t code;      /* ns_kv_code                                                       */
-  int64_t stride_b, stride_h, stride_t; /* strides of k and v in bytes: multiples of 16, not negative, stride_t >= D
-                        (calls that only read take 0 too: sequences that share what they hold)   */
+  int64_t stride_b, stride_h, stride_t; /* strides of k and v in bytes: multiples of 16, not negative, D <= stride_t
+                        <= 2^25 (calls that only read take stride_b = 0: sequences that share what they hold) */
   void *k, *v;                /* codes, 16-byte aligned; the D codes of a token are contiguous   */
   float *k_scale, *v_scale;   /* [B, heads_kv, capacity / block]                         */
 } ns_kv_cache;

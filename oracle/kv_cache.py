@@ -60,12 +60,12 @@ def append(codes, scale, x, start, counts, code):
 
 
 def attend(q, k, v, lengths, counts, scale, causal):
-    """out [B,Hq,T,D], lse [B,Hq,T], weights [B,H,N] (this call's), and two sizes that bound rounding errors:
-    the sum of |p v| like out, and the largest scale * sum |q k| of each row like lse."""
+    """out [B,Hq,T,D], lse [B,Hq,T], weights [B,H,N] (this call's), and three sizes that bound rounding errors:
+    the sum of |p v| like out, the largest scale * sum |q k| of each row like lse, and the sum of |v| over a row's keys like out."""
     B, Hq, T, D = q.shape
     H, N = k.shape[1], k.shape[2]
     G = Hq // H
-    out, spread = np.zeros((B, Hq, T, D)), np.zeros((B, Hq, T, D))
+    out, spread, volume = (np.zeros((B, Hq, T, D)) for _ in range(3))
     lse, reach = np.full((B, Hq, T), -np.inf), np.zeros((B, Hq, T))
     weights = np.zeros((B, H, N))
     for b in range(B):
@@ -83,10 +83,11 @@ def attend(q, k, v, lengths, counts, scale, causal):
             p /= total[:, None]
             out[b, hq, :c] = p @ v[b, h, :n]
             spread[b, hq, :c] = p @ np.abs(v[b, h, :n])
+            volume[b, hq, :c] = seen @ np.abs(v[b, h, :n])
             reach[b, hq, :c] = (np.abs(scale) * (np.abs(q[b, hq, :c]) @ np.abs(k[b, h, :n]).T) * seen).max(1)
             lse[b, hq, :c] = np.where(some, most + np.log(total), -np.inf)
             weights[b, h, :n] += p.sum(0)
-    return out, lse, weights, spread, reach
+    return out, lse, weights, spread, reach, volume
 
 
 def select(weights, length, keep, n_global, n_recent):

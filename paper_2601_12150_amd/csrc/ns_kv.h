@@ -23,6 +23,9 @@ ns_status launch_kv_read(const ns_kv_cache &c, const int32_t *lengths, int first
                          hipStream_t s);
 size_t kv_attn_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights);
 ns_status launch_kv_attn(const KvAttnArgs &a);
+// ... of many rows per key/value head (ns_kv_prompt.hip)
+size_t kv_prompt_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights);
+ns_status launch_kv_prompt(const KvAttnArgs &a);
 size_t kv_evict_workspace_bytes(const ns_kv_cache &from, int keep);
 ns_status launch_kv_evict(const ns_kv_cache &from, const ns_kv_cache &to, const float *weights, const int32_t *lengths, int keep,
                           int n_global, int n_recent, int32_t *kept, float *w_out, int32_t *lengths_out, void *ws, hipStream_t s);

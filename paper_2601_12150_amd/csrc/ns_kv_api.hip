@@ -20,6 +20,7 @@ ns_status validate_cache(const ns_kv_cache *c) {
   if (c->capacity > (1 << 30)) return fail(NS_ERR_UNSUPPORTED, "capacity above 2^30");
   if (c->batch > 65535) return fail(NS_ERR_UNSUPPORTED, "batch above 65535");
   if (c->heads_kv > 1024) return fail(NS_ERR_UNSUPPORTED, "more than 1024 key/value heads");
+  if (c->stride_t > (1 << 25)) return fail(NS_ERR_UNSUPPORTED, "tokens more than 2^25 bytes apart");
   if (c->stride_t < c->head_dim || c->stride_t % 16 || c->stride_h % 16 || c->stride_b % 16 || c->stride_h < 0 || c->stride_b < 0)
     return fail(NS_ERR_INVALID_ARG, "the cache's strides must be non-negative multiples of 16 bytes, stride_t >= head_dim");
   return NS_OK;

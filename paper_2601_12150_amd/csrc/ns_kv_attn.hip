@@ -1,7 +1,7 @@
 // Attention over the 8-bit key/value cache for few query rows per key/value head (single tokens of a group of heads, a few
 // drafted tokens): bound by the reads of the cache.
 //
-// The rows of a key/value head, r = (head in the group) * tokens + t, are the columns of the products
+// The rows of a key/value head, r = token * group + head in the group, are the columns of the products
 //     S^T = K Q^T   (16 keys x 32 channels  by  32 channels x 16 rows)
 //     O^T = V^T P^T (16 channels x 32 keys  by  32 keys x 16 rows)
 // so that a lane of the result of the first one holds logits of one row for four keys of every 16, and 32 keys' weights
@@ -20,7 +20,9 @@ namespace ns {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kSub = 32, kTile = kWaves * kSub;
-constexpr float kLift = 8.f, kRoom = 15.f;        // weights are 2^(z - m + 8): at most 2^15 in fp16 before m is moved up
+// Weights are 2^(z - m + 11) in fp16, m a logit near the largest so far, which is moved up before they pass 2^15: a weight that is the
+// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.
+constexpr float kLift = 11.f, kRoom = 15.f;
 
 struct Span { int64_t lo, hi; };                  // tiles of this workgroup
 
@@ -111,10 +113,11 @@ __global__ __launch_bounds__(kThreads, NT * D <= 128 ? 2 : 1) void kv_attn_split
     int limit[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-      const int r = nt * 16 + n16, t = r % d.tokens;
+      const int r = nt * 16 + n16;
       const bool real = r < R;
+      const int t = real ? r / G : 0;
       limit[nt] = real ? kv_seen(d, t, length, count) : 0;
-      const T *p = q + b * d.q_stride_b + (int64_t)(h * G + (real ? r / d.tokens : 0)) * d.q_stride_h + (int64_t)(real ? t : 0) * d.q_stride_t;
+      const T *p = q + b * d.q_stride_b + (int64_t)(h * G + (real ? r - t * G : 0)) * d.q_stride_h + (int64_t)t * d.q_stride_t;
       f32x4 x[D / 16];
       uint32_t most = 0;
 #pragma unroll
@@ -373,7 +376,8 @@ __global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, n
     }
     const bool some = M != -INFINITY;
     const float inv = some ? 1.f / L : 0.f;
-    T *to = out + b * d.out_stride_b + (int64_t)(h * G + r / d.tokens) * d.out_stride_h + (int64_t)(r % d.tokens) * d.out_stride_t + dd;
+    const int t = r / G, hq = h * G + r - t * G;
+    T *to = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd;
 #pragma unroll
     for (int e = 0; e < 4; e++) a[e] = some ? a[e] * inv : 0.f;
     if constexpr (sizeof(T) == 4) {
@@ -383,7 +387,7 @@ __global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, n
     }
     if (tid == 0) {
       const float z2 = some ? M + __log2f(L) : -INFINITY;
-      if (lse) lse[((int64_t)b * d.heads + h * G) * d.tokens + r] = z2 * kLn2;
+      if (lse) lse[((int64_t)b * d.heads + hq) * d.tokens + t] = z2 * kLn2;
       if (lse2) lse2[row * R + r] = z2;
     }
   }
@@ -392,14 +396,15 @@ __global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, n
 // The weights that every position was given, from the rows' logits; four positions a thread.
 __global__ __launch_bounds__(kThreads) void kv_weights_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
                                                               const float *logits, const float *lse2, const float *w_in, float *w_out) {
-  const int h = blockIdx.y, b = blockIdx.z, n0 = (int)(blockIdx.x * kThreads + threadIdx.x) * 4, R = d.heads / c.heads_kv * d.tokens;
+  const int h = blockIdx.y, b = blockIdx.z, n0 = (int)(blockIdx.x * kThreads + threadIdx.x) * 4;
+  const int G = d.heads / c.heads_kv, R = G * d.tokens;
   const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
   if (n0 >= c.capacity || (n0 >= length && w_in == w_out)) return;
   const int64_t row = (int64_t)b * c.heads_kv + h;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   if (n0 < length)
     for (int r = 0; r < R; r++) {
-      const int limit = kv_seen(d, r % d.tokens, length, count);
+      const int limit = kv_seen(d, r / G, length, count);
       const f32x4 z = *reinterpret_cast<const f32x4 *>(logits + (row * R + r) * c.capacity + n0);
       const float ref = lse2[row * R + r];
 #pragma unroll
@@ -410,107 +415,6 @@ __global__ __launch_bounds__(kThreads) void kv_weights_kernel(ns_kv_cache c, ns_
     if (n0 + i < length || w_in != w_out) w_out[at + i] = (w_in ? w_in[at + i] : 0.f) + sum[i];
 }
 
-// ---- the simple row kernel (many rows)
-
-template <int CODE>
-__device__ __forceinline__ float dot_codes(const float *q, const uint8_t *codes, int D) {
-  float a = 0.f;
-  for (int d = 0; d < D; d += 16) {
-    const u32x4 w = *reinterpret_cast<const u32x4 *>(codes + d);
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const f32x4 c = kv_decode4<CODE>(w[i]);
-#pragma unroll
-      for (int j = 0; j < 4; j++) a = __builtin_fmaf(q[d + 4 * i + j], c[j], a);
-    }
-  }
-  return a;
-}
-
-template <typename T> __device__ __forceinline__ T to_out(float x);
-template <> __device__ __forceinline__ float to_out<float>(float x) { return x; }
-template <> __device__ __forceinline__ bf16_t to_out<bf16_t>(float x) { return (bf16_t)x; }
-
-__device__ __forceinline__ float group_max(float x, float *tmp, int tid) {
-  x = wave_max(x);
-  __syncthreads();
-  if (tid % 64 == 0) tmp[tid / 64] = x;
-  __syncthreads();
-  return fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
-}
-
-template <typename T, int CODE>
-__global__ __launch_bounds__(kThreads) void kv_attn_row_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
-                                                               const int32_t *counts, T *out, float *lse) {
-  const int t = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, D = c.head_dim;
-  const int h = hq / (d.heads / c.heads_kv);
-  const int limit = kv_seen(d, t, kv_length(lengths, b, c.capacity), kv_count(counts, b, d.tokens));
-  const uint8_t *k = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
-  const uint8_t *v = static_cast<const uint8_t *>(c.v) + b * c.stride_b + h * c.stride_h;
-  const int64_t blocks = ((int64_t)b * c.heads_kv + h) * (c.capacity / c.block);
-  __shared__ float row[256], p[kThreads], tmp[4];
-  if (tid < D) row[tid] = (float)q[b * d.q_stride_b + hq * d.q_stride_h + t * d.q_stride_t + tid];
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int at = 0; at < limit; at += kThreads) {
-    const int n = at + tid;
-    const float z = n < limit ? dot_codes<CODE>(row, k + n * c.stride_t, D) * (c.k_scale[blocks + n / c.block] * d.scale) : -INFINITY;
-    const float next = fmaxf(m, group_max(z, tmp, tid));
-    const float ref = next == -INFINITY ? 0.f : next, fade = __expf(m - ref);
-    p[tid] = z == -INFINITY ? 0.f : __expf(z - ref);
-    __syncthreads();
-    l *= fade;
-    o *= fade;
-    const int here = min(kThreads, limit - at);
-    for (int j = 0; j < here; j++) {
-      l += p[j];
-      if (tid < D) {
-        const uint32_t w = v[(at + j) * c.stride_t + tid];
-        o = __builtin_fmaf(p[j] * c.v_scale[blocks + (at + j) / c.block], kv_decode4<CODE>(w)[0], o);
-      }
-    }
-    m = next;
-  }
-  if (tid < D) out[b * d.out_stride_b + hq * d.out_stride_h + t * d.out_stride_t + tid] = to_out<T>(limit ? o / l : 0.f);
-  if (tid == 0 && lse) lse[((int64_t)b * d.heads + hq) * d.tokens + t] = limit ? m + __logf(l) : -INFINITY;
-}
-
-// One thread per position: the sum over all rows that read its head.
-template <typename T, int CODE>
-__global__ __launch_bounds__(kThreads) void kv_weights_row_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
-                                                              const int32_t *counts, const float *lse, const float *w_in, float *w_out) {
-  const int n = blockIdx.x * kThreads + threadIdx.x, h = blockIdx.y, b = blockIdx.z, D = c.head_dim, G = d.heads / c.heads_kv;
-  const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
-  __shared__ float row[256];
-  float sum = 0.f;
-  for (int g = 0; g < G; g++)
-    for (int t = 0; t < count; t++) {
-      __syncthreads();
-      if ((int)threadIdx.x < D) row[threadIdx.x] = (float)q[b * d.q_stride_b + (h * G + g) * d.q_stride_h + t * d.q_stride_t + threadIdx.x];
-      __syncthreads();
-      if (n < kv_seen(d, t, length, count)) {
-        const float s = c.k_scale[((int64_t)b * c.heads_kv + h) * (c.capacity / c.block) + n / c.block] * d.scale;
-        sum += __expf(dot_codes<CODE>(row, static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h + n * c.stride_t, D) * s -
-                      lse[((int64_t)b * d.heads + h * G + g) * d.tokens + t]);
-      }
-    }
-  const int64_t at = ((int64_t)b * c.heads_kv + h) * c.capacity + n;
-  if (n < c.capacity && (n < length || w_in != w_out)) w_out[at] = (w_in ? w_in[at] : 0.f) + sum;
-}
-
-template <typename T, int CODE>
-ns_status launch_rows(const KvAttnArgs &a) {
-  const T *q = static_cast<const T *>(a.q);
-  float *lse = a.lse ? a.lse : reinterpret_cast<float *>(a.ws);
-  hipLaunchKernelGGL((kv_attn_row_kernel<T, CODE>), dim3((unsigned)a.d.tokens, (unsigned)a.d.heads, (unsigned)a.c.batch), dim3(kThreads), 0,
-                     a.stream, a.c, a.d, q, a.lengths, a.counts, static_cast<T *>(a.out), lse);
-  const ns_status st = check_launch("kv_attn_row_kernel");
-  if (st != NS_OK || !a.w_out) return st;
-  hipLaunchKernelGGL((kv_weights_row_kernel<T, CODE>), dim3((unsigned)((a.c.capacity + kThreads - 1) / kThreads), (unsigned)a.c.heads_kv, (unsigned)a.c.batch),
-                     dim3(kThreads), 0, a.stream, a.c, a.d, q, a.lengths, a.counts, lse, a.w_in, a.w_out);
-  return check_launch("kv_weights_row_kernel");
-}
-
 // ---- host side of the split kernel
 
 int rows_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return d.heads / c.heads_kv * d.tokens; }
@@ -518,7 +422,7 @@ int rows_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return d.heads / c
 // Row tiles of 16 that the split kernel has registers for
 int most_tiles(int head_dim, int dtype) {
   if (dtype == NS_F32) return head_dim == 64 ? 4 : head_dim == 128 ? 2 : 1;
-  return head_dim == 256 ? 2 : 4;
+  return head_dim == 256 ? 1 : 4;
 }
 bool few_rows(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return rows_of(c, d) <= 16 * most_tiles(c.head_dim, d.dtype); }
 
@@ -560,7 +464,7 @@ ns_status launch_split(const KvAttnArgs &a) {
 
 template <typename T, int CODE, int D>
 ns_status launch_tiles(const KvAttnArgs &a) {
-  constexpr int most = sizeof(T) == 4 ? (D == 64 ? 4 : D == 128 ? 2 : 1) : D == 256 ? 2 : 4;
+  constexpr int most = sizeof(T) == 4 ? (D == 64 ? 4 : D == 128 ? 2 : 1) : D == 256 ? 1 : 4;
   const int nt = (rows_of(a.c, a.d) + 15) / 16;
   if (nt <= 1) return launch_split<T, CODE, D, 1>(a);
   if constexpr (most >= 4)
@@ -571,14 +475,14 @@ ns_status launch_tiles(const KvAttnArgs &a) {
 
 template <typename T, int CODE>
 ns_status launch_any(const KvAttnArgs &a) {
-  if (!few_rows(a.c, a.d)) return launch_rows<T, CODE>(a);
+  if (!few_rows(a.c, a.d)) return launch_kv_prompt(a);
   return a.c.head_dim == 64 ? launch_tiles<T, CODE, 64>(a) : a.c.head_dim == 128 ? launch_tiles<T, CODE, 128>(a) : launch_tiles<T, CODE, 256>(a);
 }
 
 }  // namespace
 
 size_t kv_attn_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
-  if (!few_rows(c, d)) return weights ? align_up((size_t)c.batch * d.heads * d.tokens * 4, 256) : 0;
+  if (!few_rows(c, d)) return kv_prompt_workspace_bytes(c, d, weights);
   return split_layout(c, d, weights).total;
 }
 

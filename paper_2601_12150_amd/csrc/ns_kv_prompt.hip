@@ -1,0 +1,650 @@
+// Attention over the 8-bit key/value cache for many query rows per key/value head (prompts, drafts of large groups): bound by the
+// products and the exponentials.
+//
+// The products are those of ns_kv_attn.hip with tiles of 32 x 32: S^T = K Q^T, O^T = V^T P^T, so that a lane of S^T holds one row's
+// logits of 32 keys in groups of four, which are P^T's operand as they stand.  A workgroup's waves have 32 rows each and share tiles of
+// 64 keys, whose codes are turned into fp16 once, on the way into LDS: K as [key][channel], V as [channel][key] with the keys in the
+// order that P^T has them.  Both have their 16-byte pieces exchanged by the row's number, so that reads and writes meet all banks.
+// While a tile is worked on, the next one's codes are written to the other half of the LDS and those after it are loaded.
+//
+// Rows are numbered r = token * group + head, so that a causal row tile ends after few more keys than it begins with.
+#include "ns_kv.h"
+#include <algorithm>
+#include <type_traits>
+
+namespace ns {
+
+namespace {
+
+constexpr int kKeys = 64;
+// Weights are 2^(z - m + 11) in fp16, m a logit near the largest so far, which is moved up before they pass 2^15: a weight that is the
+// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.
+constexpr float kLift = 11.f, kRoom = 15.f;
+
+typedef __attribute__((address_space(3))) uint8_t lds_t;
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+}
+template <typename T> __device__ __forceinline__ f32x4 load4(const T *p);
+template <> __device__ __forceinline__ f32x4 load4<float>(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+template <> __device__ __forceinline__ f32x4 load4<bf16_t>(const bf16_t *p) {
+  const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+  return f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
+}
+
+// 16-byte pieces of a row of K (D / 8 of them) and of V^T (8) in LDS.  V^T's rows are written four channels apart and read one
+// apart: the exchange of its pieces is one to one in bits 0..2 of the channel as well as in bits 2..4.  Exchanges are exclusive ors, so
+// that of another piece of the row the address is another exclusive or.
+template <int D> __device__ __forceinline__ uint32_t k_at(int key, int piece) {
+  return (uint32_t)(key * D * 2 + ((piece ^ (key & (D == 64 ? 7 : 15))) * 16));
+}
+__device__ __forceinline__ uint32_t v_at(int channel, int piece) {
+  return (uint32_t)(channel * kKeys * 2 + ((piece ^ ((channel & 7) ^ ((channel >> 3) & 3))) * 16));
+}
+// 2^x exactly, 2^-10 <= s <= 2^7: what V's codes are multiplied with in fp16 without a rounding (e4m3's least code is 2^-9, of 3 bits)
+__device__ __forceinline__ bool plain_ratio(float s) {
+  const uint32_t u = __float_as_uint(s);
+  return (u & 0x7fffffu) == 0 && u >= (117u << 23) && u <= (134u << 23);
+}
+
+// What a launch leaves for the joins and for the weights' pass: records [split][head][row], and the rows' operands.
+struct PromptArgs {
+  float *part_o, *part_ml;         // splits > 1: [splits][B Hkv][R] D floats / (reference, sum)
+  float *lse2;                     // nullable [B Hkv][R]: log2 of the sum, +inf for a row that sees nothing
+  int splits;
+};
+
+// DV: channels of V, and of out, that a workgroup takes: all, or half of them (fp32, D = 256: registers; the logits are computed twice)
+template <typename T, int CODE, int D, int DV, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
+                                                               const int32_t *counts, T *out, float *lse, PromptArgs a) {
+  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = DV / 32, ROWS = WAVES * 32, THREADS = WAVES * 64;
+  constexpr uint32_t kV = kKeys * D * 2, kHalf = kV + kKeys * DV * 2;   // bytes of a tile's K, and with its V^T
+  // Registers for both parts of the queries, and LDS for two tiles?  fp32 with D = 256 has the second part in LDS, and one tile.
+  constexpr bool EARLY = PARTS * D < 512;
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n32 = lane & 31, hh = lane >> 5;
+  const int G = d.heads / c.heads_kv, R = G * d.tokens;
+  const int tiles = (R + ROWS - 1) / ROWS;
+  // the last rows see most: they go first
+  const int part = (int)blockIdx.x % (D / DV), x_tile = (int)blockIdx.x / (D / DV);
+  const int tile = tiles - 1 - x_tile / a.splits, split = x_tile % a.splits, h = blockIdx.y, b = blockIdx.z;
+  const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
+  const int64_t row = (int64_t)b * c.heads_kv + h;
+
+  const int r = tile * ROWS + wave * 32 + n32;
+  const bool real = r < R;
+  const int t = real ? r / G : 0, hq = h * G + (real ? r - t * G : 0);
+  const int limit = real ? kv_seen(d, t, length, count) : 0;
+  // the keys of this workgroup: those that some row sees, or its part of them
+  const int last_t = min(min(tile * ROWS + ROWS, R) - 1, R - 1) / G;
+  int seen = d.causal ? kv_seen(d, min(last_t, count - 1), length, count) : length;
+  if (tile * ROWS / G >= count) seen = 0;
+  int n_lo = 0, n_hi = seen;
+  if (a.splits > 1) {
+    const int share = ((seen + a.splits - 1) / a.splits + kKeys - 1) / kKeys * kKeys;
+    n_lo = min(split * share, seen);
+    n_hi = min(n_lo + share, seen);
+  }
+  // of the wave: the keys that all its rows see, and those that any of them sees
+  int every = real ? limit : 0x7fffffff, any = limit;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    every = min(every, __shfl_xor(every, o));
+    any = max(any, __shfl_xor(any, o));
+  }
+  every = __builtin_amdgcn_readfirstlane(every);
+  any = __builtin_amdgcn_readfirstlane(any);
+
+  // ---- queries
+  Frag qf[PARTS][KS];
+  float factor;
+  {
+    const T *p = q + b * d.q_stride_b + (int64_t)hq * d.q_stride_h + (int64_t)t * d.q_stride_t + 8 * hh;
+    uint32_t most = 0;
+#pragma unroll
+    for (int s = 0; s < KS; s++)
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const f32x4 x = load4(p + 16 * s + 4 * i);
+#pragma unroll
+        for (int j = 0; j < 4; j++) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+      }
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+    const int shift = kv_row_shift(most);
+    factor = real ? ldexpf(d.scale * kLog2e, -shift) : 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; s++)
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const f32x4 x = load4(p + 16 * s + 4 * i);
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const float x0 = real ? ldexpf(x[j], shift) : 0.f, x1 = real ? ldexpf(x[j + 1], shift) : 0.f;
+          const uint32_t hi = pack_f16(x0, x1);
+          qf[0][s].w[2 * i + j / 2] = hi;
+          if (PARTS == 2) {
+            const f16x2 w = __builtin_bit_cast(f16x2, hi);
+            qf[PARTS - 1][s].w[2 * i + j / 2] = pack_f16(x0 - (float)w[0], x1 - (float)w[1]);
+          }
+        }
+      }
+  }
+
+  uint8_t *q_lds = lds + kHalf + (wave * KS * 64 + lane) * 16;
+  if constexpr (!EARLY) {
+#pragma unroll
+    for (int s = 0; s < KS; s++) *reinterpret_cast<f16x8 *>(q_lds + s * 1024) = qf[PARTS - 1][s].v;
+  }
+
+  // ---- codes on their way into LDS
+  const uint8_t *kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
+  const uint8_t *vb = static_cast<const uint8_t *>(c.v) + b * c.stride_b + h * c.stride_h + part * DV;
+  const float *ks = c.k_scale + row * (c.capacity / c.block), *vs = c.v_scale + row * (c.capacity / c.block);
+  const int lblock = 31 - __clz(c.block);
+  constexpr int KP = kKeys * D / 16 / THREADS, VP = kKeys / 4 * (DV / 4) / THREADS;      // pieces a thread has of K (16 codes) and V (4 x 4)
+  constexpr int KR = THREADS / (D / 16), VR = THREADS / (DV / 4) * 4;                    // keys between two of its pieces
+  const int k_key = tid / (D / 16), v_key = tid / (DV / 4) * 4;
+  const uint32_t stride = (uint32_t)c.stride_t;
+  u32x4 kraw[KP];
+  uint32_t vraw[VP][4];
+  auto fetch = [&](int n0) {
+    const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
+    const int most = c.capacity - 1 - n0;           // (the last tile of blocks of 32 may reach beyond the capacity)
+#pragma unroll
+    for (int i = 0; i < KP; i++) kraw[i] = *reinterpret_cast<const u32x4 *>(kp + ((uint32_t)min(k_key + i * KR, most) * stride + tid % (D / 16) * 16));
+#pragma unroll
+    for (int i = 0; i < VP; i++)
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        vraw[i][j] = *reinterpret_cast<const uint32_t *>(vp + ((uint32_t)min(v_key + i * VR + j, most) * stride + tid % (DV / 4) * 4));
+  };
+  // V's scales: o is in units of `unit`, a tile's V in LDS in units of `next`, which is the same but where a much larger scale
+  // comes along.  Where both halves' scales are next times a plain ratio, V is multiplied by that on its way (slow = false); else (a NaN, far
+  // smaller ones, the caller's own that are no powers of two) LDS has the bare codes, and the products are multiplied.
+  float unit = 0.f, next = 0.f, rel0 = 1.f, rel1 = 1.f;
+  bool slow = false;
+  auto stage = [&](int n0, uint32_t at) {
+    const int n1 = min(n0 + 32, c.capacity - 32);
+    const float s0 = vs[n0 >> lblock], s1 = n0 + 32 < length ? vs[n1 >> lblock] : s0, big = fmaxf(s0, s1);
+    if (!(big <= next * 0x1p7f) && big > 0.f && big < INFINITY) next = big;      // (the first tile's too)
+    rel0 = s0 / next;
+    rel1 = s1 / next;
+    slow = !EARLY || !(plain_ratio(rel0) && plain_ratio(rel1));
+    const _Float16 h0 = (_Float16)(slow ? 1.f : rel0), h1 = (_Float16)(slow ? 1.f : rel1);
+    // (opaque: else the compiler keeps every address in a register of its own)
+    const uint32_t k_to = (uint32_t)opaque((int)(at + k_at<D>(k_key, tid % (D / 16) * 2)));
+    const int quad0 = v_key / 4;
+    const uint32_t v_to = (uint32_t)opaque((int)(at + kV + v_at(tid % (DV / 4) * 4, (quad0 >> 2) * 2 + (quad0 & 1)) + ((quad0 >> 1) & 1) * 8));
+#pragma unroll
+    for (int i = 0; i < KP; i++) {
+      const uint32_t to = k_to + i * KR * D * 2;
+      static_assert(KR % 16 == 0 || KP == 1, "the exchange is the same for all of a thread's pieces");
+      *reinterpret_cast<f16x8 *>(lds + to) = kv_frag<CODE>(kraw[i][0], kraw[i][1]).v;
+      *reinterpret_cast<f16x8 *>(lds + (to ^ 16)) = kv_frag<CODE>(kraw[i][2], kraw[i][3]).v;
+    }
+    const bool tail = n0 + kKeys > length;         // what lies behind may be NaN
+#pragma unroll
+    for (int i = 0; i < VP; i++) {
+      const int key = v_key + i * VR;
+      static_assert(VP == 1 || VR == 16 || VR == 32, "a thread's keys are 16 or 32 apart: two or four pieces further on");
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; j++) w[j] = kv_raw<CODE>(tail && n0 + key + j >= length ? 0u : vraw[i][j]);
+      const uint32_t lo0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+      const uint32_t hi0 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+      const _Float16 f = key >= 32 ? h1 : h0;
+      auto times = [&](uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * f16x2{f, f}); };
+      // keys 4 quad .. + 3 are the first or second half of the piece that lanes of half (quad & 1) read for the step quad / 4
+      const uint32_t to = v_to ^ (uint32_t)(VR * 2 * i);
+      *reinterpret_cast<u32x2 *>(lds + to) = u32x2{times(kv_f16x2<CODE, 0>(lo0)), times(kv_f16x2<CODE, 0>(lo1))};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 16) + kKeys * 2) = u32x2{times(kv_f16x2<CODE, 1>(lo0)), times(kv_f16x2<CODE, 1>(lo1))};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 32) + kKeys * 4) = u32x2{times(kv_f16x2<CODE, 0>(hi0)), times(kv_f16x2<CODE, 0>(hi1))};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 48) + kKeys * 6) = u32x2{times(kv_f16x2<CODE, 1>(hi0)), times(kv_f16x2<CODE, 1>(hi1))};
+    }
+  };
+
+  f32x16 o[MT];
+#pragma unroll
+  for (int i = 0; i < MT; i++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) o[i][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  uint32_t at = 0;
+  const uint32_t k_lane = k_at<D>(n32, hh), v_lane = kV + v_at(n32, hh);
+  int n0 = n_lo;
+  // one tile: its logits, weights and values.  SLOW: its V holds bare codes
+  auto tile_of_keys = [&](auto is_slow, float f_v0, float f_v1, float tile_unit) {
+    constexpr bool SLOW = decltype(is_slow)::value;
+    const bool edge = n0 + kKeys > every;
+    const uint32_t kl = (uint32_t)opaque((int)(k_lane + at)), vl = (uint32_t)opaque((int)(v_lane + at));
+    f32x16 s[2];
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[x][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        const f16x8 kf = *reinterpret_cast<const f16x8 *>(lds + (kl ^ (32u * k)) + x * 32 * D * 2);
+#pragma unroll
+        for (int pt = PARTS - 1; pt >= 0; pt--) {
+          const f16x8 qv = pt == 1 && !EARLY ? *reinterpret_cast<const f16x8 *>(q_lds + k * 1024) : qf[pt][k].v;
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qv, s[x], 0, 0, 0);
+        }
+        if (!EARLY && k % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (not all operands at once)
+      }
+    }
+    const int n1 = min(n0 + 32, c.capacity - 32);     // (behind the capacity: masked, any scale will do)
+    const float sk[2] = {ks[n0 >> lblock], ks[n1 >> lblock]};
+    const bool fresh = m == -INFINITY;
+    const float ref = fresh ? 0.f : m;
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+      const float f = factor * sk[x];
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        float z = __builtin_fmaf(s[x][e], f, -ref);
+        if (edge) z = n0 + x * 32 + (e >> 2) * 8 + hh * 4 + (e & 3) < limit ? z : -INFINITY;
+        s[x][e] = z;
+        top = fmaxf(top, z);
+      }
+    }
+    if (__any(top > kRoom || (fresh && top > -INFINITY)) || tile_unit != unit) {
+      top = half_swap_max(top);
+      const bool moved = top > kRoom || (fresh && top > -INFINITY);
+      const float move = moved ? top - kLift : 0.f;
+      float fade = __builtin_amdgcn_exp2f(-move);
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[x][e] -= move;
+      if (moved) m = ref + move;
+      l *= fade;
+      fade *= unit / tile_unit;
+      unit = tile_unit;
+#pragma unroll
+      for (int i = 0; i < MT; i++) o[i] *= fade;
+    }
+    Frag pf[PARTS][4];
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(s[x][e]), p1 = __builtin_amdgcn_exp2f(s[x][e + 1]);
+        l += p0;
+        l += p1;
+        const uint32_t hi = pack_f16(p0, p1);
+        pf[0][x * 2 + e / 8].w[e % 8 / 2] = hi;
+        if (PARTS == 2) {
+          const f16x2 w = __builtin_bit_cast(f16x2, hi);
+          pf[PARTS - 1][x * 2 + e / 8].w[e % 8 / 2] = pack_f16(p0 - (float)w[0], p1 - (float)w[1]);
+        }
+      }
+    if constexpr (!SLOW) {
+#pragma unroll
+      for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          const f16x8 vf = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)) + i * 32 * kKeys * 2);
+#pragma unroll
+          for (int pt = PARTS - 1; pt >= 0; pt--) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[pt][k].v, o[i], 0, 0, 0);
+        }
+    } else {                                          // (a NaN block makes those rows NaN that see it)
+      const float f0 = edge && n0 >= limit ? 0.f : f_v0, f1 = edge && n0 + 32 >= limit ? 0.f : f_v1;
+#pragma unroll
+      for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          f32x16 y;
+#pragma unroll
+          for (int e = 0; e < 16; e++) y[e] = 0.f;
+#pragma unroll
+          for (int k = 2 * x; k < 2 * x + 2; k++) {
+            const f16x8 vf = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)) + i * 32 * kKeys * 2);
+#pragma unroll
+            for (int pt = PARTS - 1; pt >= 0; pt--) y = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[pt][k].v, y, 0, 0, 0);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; e++) o[i][e] = __builtin_fmaf(y[e], x ? f1 : f0, o[i][e]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  };
+  auto ahead = [&] {                                  // the next tile into the other half, the one after it on its way
+    if (EARLY && n0 + kKeys < n_hi) {
+      stage(n0 + kKeys, at ^ kHalf);
+      if (n0 + 2 * kKeys < n_hi) fetch(n0 + 2 * kKeys);
+    }
+  };
+  auto step = [&] {
+    __syncthreads();
+    if (EARLY) at ^= kHalf;
+    n0 += kKeys;
+    if (!EARLY && n0 < n_hi) {
+      fetch(n0);
+      stage(n0, at);
+      __syncthreads();
+    }
+  };
+  if (n_lo < n_hi) {
+    fetch(n_lo);
+    stage(n_lo, 0);
+    unit = next;
+    if (EARLY && n_lo + kKeys < n_hi) fetch(n_lo + kKeys);
+    __syncthreads();
+  }
+  // (loops of their own for the two kinds of tiles, and for those that the wave has no part in: o stays in its registers)
+  const int n_wave = min(n_hi, any);
+  while (n0 < n_wave) {
+    if constexpr (EARLY)
+      while (n0 < n_wave && !slow) {
+        const float u = next;
+        ahead();
+        tile_of_keys(std::false_type{}, 0.f, 0.f, u);
+        step();
+      }
+    while (n0 < n_wave && slow) {
+      const float u = next, f0 = rel0, f1 = rel1;
+      ahead();
+      tile_of_keys(std::true_type{}, f0, f1, u);
+      step();
+    }
+  }
+  while (n0 < n_hi) {
+    ahead();
+    step();
+  }
+
+  // ---- out: a lane has its row's channels 32 i + 8 (e / 4) + 4 hh + e % 4
+  l = half_swap_sum(l);
+  if (m == -INFINITY && l != l) m = 0.f;            // a row of NaN is not an empty one
+  if (!real) return;
+  if (a.splits > 1) {
+    const int64_t rec = ((int64_t)split * c.batch * c.heads_kv + row) * R + r;
+    const float u = unit;
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4 *>(a.part_o + rec * D + part * DV + 32 * i + 2 * e + 4 * hh) = f32x4{o[i][e] * u, o[i][e + 1] * u, o[i][e + 2] * u, o[i][e + 3] * u};
+    if (hh == 0 && part == 0) *reinterpret_cast<f32x2 *>(a.part_ml + rec * 2) = f32x2{m, l};
+    return;
+  }
+  const bool some = m != -INFINITY;
+  const float by = some ? unit / l : 0.f;
+  T *to = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + part * DV;
+#pragma unroll
+  for (int i = 0; i < MT; i++)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      f32x4 y;
+#pragma unroll
+      for (int j = 0; j < 4; j++) y[j] = some ? o[i][e + j] * by : 0.f;
+      T *p = to + 32 * i + 2 * e + 4 * hh;
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<f32x4 *>(p) = y;
+      else
+        *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    }
+  if (hh == 0 && part == 0) {
+    const float z2 = some ? m + __log2f(l) : -INFINITY;
+    if (lse) lse[((int64_t)b * d.heads + hq) * d.tokens + t] = z2 * kLn2;
+    if (a.lse2) a.lse2[row * R + r] = some ? z2 : INFINITY;
+  }
+}
+
+// One wave per row: the splits' results together.
+template <typename T>
+__global__ __launch_bounds__(256) void kv_prompt_join_kernel(ns_kv_cache c, ns_kv_attn_desc d, PromptArgs a, T *out, float *lse) {
+  const int lane = threadIdx.x & 63, D = c.head_dim, G = d.heads / c.heads_kv, R = G * d.tokens;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
+  if (r >= R) return;
+  const int64_t heads = (int64_t)c.batch * c.heads_kv, row = (int64_t)b * c.heads_kv + h;
+  float M = -INFINITY;
+  for (int s = 0; s < a.splits; s++) M = fmaxf(M, a.part_ml[((s * heads + row) * R + r) * 2]);
+  const int dd = lane * 4, n = D / 4;                // D = 256: all lanes
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  float L = 0.f;
+  for (int s = 0; s < a.splits; s++) {
+    const int64_t rec = (s * heads + row) * R + r;
+    const float ms = a.part_ml[rec * 2];
+    if (ms == -INFINITY) continue;
+    const float fade = __builtin_amdgcn_exp2f(ms - M);
+    L += a.part_ml[rec * 2 + 1] * fade;
+    if (lane < n) y += *reinterpret_cast<const f32x4 *>(a.part_o + rec * D + dd) * fade;
+  }
+  const bool some = M != -INFINITY;
+  const int t = r / G, hq = h * G + r - t * G;
+  if (lane < n) {
+    const float inv = some ? 1.f / L : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; j++) y[j] = some ? y[j] * inv : 0.f;
+    T *p = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd;
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<f32x4 *>(p) = y;
+    else
+      *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+  }
+  if (lane == 0) {
+    const float z2 = some ? M + __log2f(L) : -INFINITY;
+    if (lse) lse[((int64_t)b * d.heads + hq) * d.tokens + t] = z2 * kLn2;
+    if (a.lse2) a.lse2[row * R + r] = some ? z2 : INFINITY;
+  }
+}
+
+// ---- the weights that every position was given: exp(logit - lse) summed over the rows, with K read again.  The rows' operands and
+// factors are made once (kv_weights_rows_kernel); a wave then has 64 keys in registers and takes 32 rows at a time from the L2.
+
+// Channels of the step s = 2 i + f that lane (n, hh) has: 32 i + 16 hh + 8 f + j, so that 16 bytes of codes are two operands.
+template <typename T>
+__global__ __launch_bounds__(256) void kv_weights_rows_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, Frag *frags, float *factors) {
+  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
+  const int lane = threadIdx.x & 63, n32 = lane & 31, hh = lane >> 5, KS = c.head_dim / 16;
+  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 31) / 32;
+  const int tile = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
+  if (tile >= tiles) return;
+  const int64_t row = (int64_t)b * c.heads_kv + h;
+  const int r = tile * 32 + n32;
+  const bool real = r < R;
+  const int t = real ? r / G : 0;
+  const T *p = q + b * d.q_stride_b + (int64_t)(h * G + (real ? r - t * G : 0)) * d.q_stride_h + (int64_t)t * d.q_stride_t + 16 * hh;
+  uint32_t most = 0;
+  for (int i = 0; i < KS / 2; i++)
+    for (int k = 0; k < 4; k++) {
+      const f32x4 x = load4(p + 32 * i + 4 * k);
+#pragma unroll
+      for (int j = 0; j < 4; j++) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+    }
+  most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+  const int shift = kv_row_shift(most);
+  if (hh == 0) factors[row * tiles * 32 + r] = real ? ldexpf(d.scale * kLog2e, -shift) : 0.f;
+  for (int s = 0; s < KS; s++) {
+    Frag f[PARTS];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      const f32x4 x = load4(p + 32 * (s / 2) + 8 * (s % 2) + 4 * k);
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const float x0 = real ? ldexpf(x[j], shift) : 0.f, x1 = real ? ldexpf(x[j + 1], shift) : 0.f;
+        f[0].w[2 * k + j / 2] = pack_f16(x0, x1);
+        if (PARTS == 2) {
+          const f16x2 w = __builtin_bit_cast(f16x2, f[0].w[2 * k + j / 2]);
+          f[PARTS - 1].w[2 * k + j / 2] = pack_f16(x0 - (float)w[0], x1 - (float)w[1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int pt = 0; pt < PARTS; pt++) frags[(((row * tiles + tile) * PARTS + pt) * KS + s) * 64 + lane] = f[pt];
+  }
+}
+
+template <int PARTS, int CODE, int D>
+__global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
+                                                             const Frag *frags, const float *factors, const float *lse2, const float *w_in,
+                                                             float *w_out) {
+  constexpr int KS = D / 16;
+  const int lane = threadIdx.x & 63, n32 = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 31) / 32;
+  const int h = blockIdx.y, b = blockIdx.z, n0 = (int)blockIdx.x * 256 + wave * 64;
+  const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
+  const int64_t row = (int64_t)b * c.heads_kv + h;
+  if (n0 >= c.capacity) return;
+  float sum = 0.f;                                  // of the key n0 + lane
+  if (n0 < length) {
+    Frag kf[2][KS];
+    float sk[2];
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+      const int key = min(n0 + 32 * x + n32, c.capacity - 1);
+      const uint8_t *p = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h + (int64_t)key * c.stride_t + 16 * hh;
+#pragma unroll
+      for (int i = 0; i < KS / 2; i++) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(p + 32 * i);
+        kf[x][2 * i] = kv_frag<CODE>(w[0], w[1]);
+        kf[x][2 * i + 1] = kv_frag<CODE>(w[2], w[3]);
+      }
+      sk[x] = c.k_scale[row * (c.capacity / c.block) + min(n0 + 32 * x, c.capacity - 32) / c.block];
+    }
+    f32x16 acc[2];
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) acc[x][e] = 0.f;
+    // causal: the first row that sees key n0 is that of the query at its position
+    const int first = d.causal ? max(0, n0 - (length - count)) * G / 32 : 0;
+    const int last = min(tiles, (count * G + 31) / 32);
+    for (int tile = first; tile < last; tile++) {
+      const int r = tile * 32 + n32;
+      const int limit = r < R ? kv_seen(d, r / G, length, count) : 0;
+      const float fr = factors[row * tiles * 32 + r], ref = r < R ? lse2[row * R + r] : INFINITY;
+      const Frag *qf = frags + ((row * tiles + tile) * PARTS) * KS * 64 + lane;
+      f32x16 s[2];
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[x][e] = 0.f;
+#pragma unroll
+      for (int pt = PARTS - 1; pt >= 0; pt--)
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+          const f16x8 qv = qf[(pt * KS + k) * 64].v;
+#pragma unroll
+          for (int x = 0; x < 2; x++) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x][k].v, qv, s[x], 0, 0, 0);
+        }
+      const bool edge = __any(n0 + 64 > limit);
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const float f = fr * sk[x];
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], f, -ref));
+          acc[x][e] += edge && n0 + 32 * x + (e >> 2) * 8 + hh * 4 + (e & 3) >= limit ? 0.f : p;
+        }
+      }
+    }
+    // over the 32 rows' lanes; lane 32 x + 8 (e / 4) + 4 hh + e % 4 takes the sum
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        float y = acc[x][e];
+        y += dpp<kDppXor1>(y);
+        y += dpp<kDppXor2>(y);
+        y += dpp<kDppMirror8>(y);
+        y += dpp<kDppMirror16>(y);
+        y = row_swap_sum(y);
+        const float other = __shfl_xor(y, 32);
+        const int at = 32 * x + (e >> 2) * 8 + (e & 3);
+        if (lane == at) sum = hh ? other : y;
+        if (lane == at + 4) sum = hh ? y : other;
+      }
+  }
+  const int n = n0 + lane;
+  if (n >= c.capacity || (n >= length && w_in == w_out)) return;
+  const int64_t at = row * c.capacity + n;
+  w_out[at] = (w_in ? w_in[at] : 0.f) + (n < length ? sum : 0.f);
+}
+
+// ---- host side
+
+constexpr int waves_of(int D) { return D == 128 ? 8 : 4; }
+
+int splits_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
+  const int64_t rows = (int64_t)d.heads / c.heads_kv * d.tokens, per = waves_of(c.head_dim) * 32;
+  const int64_t wgs = (rows + per - 1) / per * c.heads_kv * c.batch, cus = device_cu_count();
+  // as many parts of the keys as fill the chip once, of 512 keys at least
+  return (int)std::max<int64_t>(1, std::min<int64_t>({cus / wgs, (int64_t)c.capacity / 512, 64}));
+}
+
+struct Layout { size_t o, ml, lse2, frags, factors, total; int splits; };
+Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
+  Layout w;
+  w.splits = splits_of(c, d);
+  const size_t rows = (size_t)(d.heads / c.heads_kv) * d.tokens, heads = (size_t)c.batch * c.heads_kv, tiles = (rows + 31) / 32;
+  size_t off = 0;
+  w.o = off;
+  if (w.splits > 1) off += align_up(w.splits * heads * rows * c.head_dim * 4, 256);
+  w.ml = off;
+  if (w.splits > 1) off += align_up(w.splits * heads * rows * 8, 256);
+  w.lse2 = off;
+  if (weights) off += align_up(heads * rows * 4, 256);
+  w.frags = off;
+  if (weights) off += align_up(heads * tiles * 32 * c.head_dim * 2 * (d.dtype == NS_F32 ? 2 : 1), 256);
+  w.factors = off;
+  if (weights) off += align_up(heads * tiles * 32 * 4, 256);
+  w.total = off;
+  return w;
+}
+
+template <typename T, int CODE, int D>
+ns_status launch(const KvAttnArgs &a) {
+  constexpr int WAVES = waves_of(D), PARTS = sizeof(T) == 4 ? 2 : 1, DV = PARTS * D == 512 ? 128 : D;
+  const ns_kv_cache &c = a.c;
+  const Layout w = layout_of(c, a.d, a.w_out != nullptr);
+  const int rows = a.d.heads / c.heads_kv * a.d.tokens, tiles = (rows + WAVES * 32 - 1) / (WAVES * 32);
+  PromptArgs p{reinterpret_cast<float *>(a.ws + w.o), reinterpret_cast<float *>(a.ws + w.ml),
+               a.w_out ? reinterpret_cast<float *>(a.ws + w.lse2) : nullptr, w.splits};
+  // two tiles, or one and the second part of the queries
+  const int tile_lds = kKeys * (D + DV) * 2, lds = DV == D ? 2 * tile_lds : tile_lds + WAVES * 32 * D * 2;
+  const T *q = static_cast<const T *>(a.q);
+  T *out = static_cast<T *>(a.out);
+  ns_status st = reserve_lds_once(reinterpret_cast<const void *>(kv_prompt_kernel<T, CODE, D, DV, WAVES>), lds);
+  if (st != NS_OK) return st;
+  const dim3 grid((unsigned)(tiles * w.splits * (D / DV)), (unsigned)c.heads_kv, (unsigned)c.batch);
+  hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES>), grid, dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out, a.lse, p);
+  st = check_launch("kv_prompt_kernel");
+  if (st == NS_OK && w.splits > 1) {
+    hipLaunchKernelGGL((kv_prompt_join_kernel<T>), dim3((unsigned)((rows + 3) / 4), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256), 0, a.stream, c, a.d,
+                       p, out, a.lse);
+    st = check_launch("kv_prompt_join_kernel");
+  }
+  if (st != NS_OK || !a.w_out) return st;
+  Frag *frags = reinterpret_cast<Frag *>(a.ws + w.frags);
+  float *factors = reinterpret_cast<float *>(a.ws + w.factors);
+  hipLaunchKernelGGL((kv_weights_rows_kernel<T>), dim3((unsigned)((rows + 127) / 128), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256), 0, a.stream, c,
+                     a.d, q, frags, factors);
+  st = check_launch("kv_weights_rows_kernel");
+  if (st != NS_OK) return st;
+  hipLaunchKernelGGL((kv_weights_sum_kernel<PARTS, CODE, D>), dim3((unsigned)((c.capacity + 255) / 256), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256),
+                     0, a.stream, c, a.d, a.lengths, a.counts, frags, factors, p.lse2, a.w_in, a.w_out);
+  return check_launch("kv_weights_sum_kernel");
+}
+
+template <typename T, int CODE> ns_status launch_d(const KvAttnArgs &a) {
+  return a.c.head_dim == 64 ? launch<T, CODE, 64>(a) : a.c.head_dim == 128 ? launch<T, CODE, 128>(a) : launch<T, CODE, 256>(a);
+}
+
+}  // namespace
+
+size_t kv_prompt_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) { return layout_of(c, d, weights).total; }
+
+ns_status launch_kv_prompt(const KvAttnArgs &a) {
+  if (a.d.dtype == NS_F32) return a.c.code == NS_CODE_I8 ? launch_d<float, NS_CODE_I8>(a) : launch_d<float, NS_CODE_E4M3>(a);
+  return a.c.code == NS_CODE_I8 ? launch_d<bf16_t, NS_CODE_I8>(a) : launch_d<bf16_t, NS_CODE_E4M3>(a);
+}
+
+}  // namespace ns

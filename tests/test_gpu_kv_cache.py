@@ -6,8 +6,9 @@ are derived from the roundings that a row goes through:
   a logit   z: fp32 sums of D products: D 2^-24 of the sum of |q k|, its scaling and the exponential's argument 4 more
   a weight  p: twice a logit's error (its own and the normaliser's), and the steps of the sums: tiles of 32 keys are summed at a
             time, so a sum over N keys is N / 32 + 100 roundings deep at most; the weight that enters the product with V has 11 bits
-            where out is bf16 (2^-11), 21 where it is fp32 (2^-21)
-  out: the weights' errors on the sum of |p v|, and the rounding of the result (2^-8 or 2^-24)
+            where out is bf16 (2^-11), 21 where it is fp32 (2^-21).  It is in fp16, times 2^11 where it is the row's largest one: what
+            is below fp16's normal numbers is off by half its least step, 2^-25 2^-11 of the largest weight, which is at most 1
+  out: the weights' errors on the sum of |p v| and of |v|, and the rounding of the result (2^-8 or 2^-24)
 """
 import numpy as np
 import pytest
@@ -175,12 +176,12 @@ def test_read(nb, code, dtype, D, block, first, tokens):
 
 
 def check_attention(got, lse, weights, want, dtype, D, N, rows):
-    out, lse_ref, w_ref, spread, reach = want
+    out, lse_ref, w_ref, spread, reach, volume = want
     z = (D + 4) * 2.0 ** -24 * reach                             # of a logit
     p = 2 * z + (N / 32 + 100) * 2.0 ** -24                       # of a weight, relative
     half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
     bits = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -21
-    off = np.abs(f64(got) - out) - ((p + bits)[..., None] * spread + half * np.abs(out) + 1e-37)
+    off = np.abs(f64(got) - out) - ((p + bits)[..., None] * spread + 2.0 ** -36 * volume + half * np.abs(out) + 1e-37)
     assert off.max() <= 0, "out exceeds its bound by %.3g" % off.max()
     if lse is not None:
         got_lse = f64(lse)

@@ -31,7 +31,7 @@ def desc(nb, **kw):
 
 BAD_CACHE = [("batch", 0, 1), ("heads_kv", 0, 1), ("head_dim", 0, 1), ("capacity", -64, 1), ("block", 0, 1), ("code", 2, 1), ("capacity", 250, 1),
              ("stride_t", 64, 1), ("stride_t", 136, 1), ("stride_h", -16, 1), ("stride_b", 8, 1), ("head_dim", 96, 2), ("block", 16, 2), ("block", 256, 2),
-             ("batch", 65536, 2), ("heads_kv", 1025, 2)]
+             ("batch", 65536, 2), ("heads_kv", 1025, 2), ("stride_t", (1 << 25) + 16, 2)]
 
 
 def calls(nb):

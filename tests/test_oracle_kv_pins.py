@@ -30,7 +30,7 @@ def test_scales(code):
 def test_attention_is_a_masked_softmax():
     rng = np.random.default_rng(1)
     q, k, v = rng.standard_normal((1, 4, 5, 8)), rng.standard_normal((1, 2, 12, 8)), rng.standard_normal((1, 2, 12, 8))
-    out, lse, w, _, _ = oracle.attend(q, k, v, [9], [4], 0.3, True)
+    out, lse, w, _, _, _ = oracle.attend(q, k, v, [9], [4], 0.3, True)
     z = torch.from_numpy(0.3 * np.einsum("htd,hnd->htn", q[0, :, :4], k[0].repeat(2, 0)[:, :9]))
     z = z + torch.full((4, 9), -math.inf, dtype=torch.float64).triu(9 - 4 + 1)
     p = z.softmax(2)
