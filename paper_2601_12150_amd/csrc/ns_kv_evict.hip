@@ -1,155 +1,402 @@
-// Eviction from the 8-bit key/value cache by added-up weight: which tokens stay (kv_select_kernel), and their move into
-// another cache, where every block gets the scale that its tokens need (kv_move_kernel).
+// Eviction from the 8-bit key/value cache by added-up weight: which tokens stay, and their move into another cache, where every block
+// gets the scale that its tokens need.
+//
+// The tokens that stay are found by the key (an order-preserving integer image of the weight) of the last of them: digits of 11,
+// 11 and 10 bits, each from a histogram of the keys that share the digits before it (radix select).  Then all tokens with a larger
+// key stay, and of those with this very key the first ones.
+//   kv_select_kernel: caches of up to 32768 tokens; one workgroup per sequence and head has all keys in registers, one launch.
+//   kv_digit_kernel, kv_place_kernel: longer ones, a workgroup per 8192 tokens; a launch for every digit and one that places.
+//   kv_move_kernel: a workgroup per block of the new cache; its codes are read once and stay in registers until the scale is known.
 #include "ns_kv.h"
 
 namespace ns {
 
 namespace {
 
-constexpr int kSelect = 1024, kMove = 256;
+constexpr int kSelect = 1024, kWaves = kSelect / 64;
+constexpr int kBits[3] = {11, 11, 10}, kShift[3] = {21, 10, 0}, kBins = 2048;
+constexpr int kHeld = 32768;                      // tokens that one workgroup selects from
+constexpr int kChunkKeys = 8, kChunk = kSelect * kChunkKeys;
 
-// larger weight <=> larger key; -0 and +0 alike, NaN above everything.  0 is nobody's key.
+// larger weight <=> larger key; -0 and +0 alike, NaN above everything
 __device__ __forceinline__ uint32_t rank_key(float w) {
   if (!(w == w)) return 0xffffffffu;
   const uint32_t u = __float_as_uint(w + 0.f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+__device__ __forceinline__ uint32_t digit_of(uint32_t key, int pass) { return (key >> kShift[pass]) & ((1u << kBits[pass]) - 1); }
 
-// One workgroup per sequence and head: the key of the last token that stays, by four digits of 8 bits (radix select), then the
-// kept tokens in order of their positions, among equal keys the first ones.
-__global__ __launch_bounds__(kSelect) void kv_select_kernel(const float *weights, const int32_t *lengths, int capacity, int keep, int n_global,
-                                                            int n_recent, int heads_kv, int to_capacity, int32_t *kept, float *w_out,
-                                                            int32_t *lengths_out) {
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int length = kv_length(lengths, b, capacity);
-  const int64_t row = (int64_t)b * heads_kv + h;
-  const float *w = weights + row * capacity;
-  kept += row * keep;
-  w_out += row * to_capacity;
-  if (h == 0 && tid == 0) lengths_out[b] = min(length, keep);
-  if (length <= keep) {
-    for (int i = tid; i < to_capacity; i += kSelect) {
-      if (i < keep) kept[i] = i < length ? i : -1;
-      w_out[i] = i < length ? w[i] : 0.f;
-    }
-    return;
+// Counts the wave's digits.  Added-up weights crowd in few bins (most tokens get next to nothing), where one LDS atomic per lane would
+// wait for the others: the first two bins that turn up are counted with one addition each.
+__device__ __forceinline__ void count_digits(uint32_t *hist, bool in, uint32_t digit, int lane) {
+  unsigned long long rest = __ballot(in);
+#pragma unroll 1
+  for (int i = 0; i < 2 && rest; i++) {
+    const int leader = __ffsll((long long)rest) - 1;
+    const uint32_t d = (uint32_t)__builtin_amdgcn_readlane((int)digit, leader);
+    const unsigned long long same = __ballot(in && digit == d) & rest;
+    if (lane == leader) atomicAdd(&hist[d], (uint32_t)__popcll(same));
+    rest &= ~same;
   }
-  const int first = n_global, last = length - n_recent;                // the ranked ones: first <= n < last
-  __shared__ uint32_t hist[256], total[kSelect / 64], found[2];
-  uint32_t prefix = 0, mask = 0, need = (uint32_t)(keep - n_global - n_recent);
-  for (int shift = 24; need && shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int n = first + tid; n < last; n += kSelect) {
-      const uint32_t key = rank_key(w[n]);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (tid == 0) {
-      int digit = 255;
-      uint32_t above = 0;
-      while (above + hist[digit] < need) above += hist[digit--];
-      found[0] = (uint32_t)digit;
-      found[1] = need - above;
-    }
-    __syncthreads();
-    prefix |= found[0] << shift;
-    mask |= 255u << shift;
-    need = found[1];
-    __syncthreads();
-  }
-  // prefix: the key of the last token that stays; need: how many of those with this very key stay
-  uint32_t placed = 0, equal = 0;
-  const bool ranked = keep > n_global + n_recent;
-  for (int at = 0; at < length; at += kSelect) {
-    const int n = at + tid;
-    const float x = n < length ? w[n] : 0.f;
-    const bool in = n >= first && n < last;
-    const uint32_t key = rank_key(x);
-    const bool eq = ranked && in && key == prefix;
-    const unsigned long long eqs = __ballot(eq);
-    __syncthreads();
-    if (lane == 0) total[wave] = (uint32_t)__popcll(eqs);
-    __syncthreads();
-    uint32_t before = equal, all = 0;
-    for (int i = 0; i < kSelect / 64; i++) {
-      before += i < wave ? total[i] : 0u;
-      all += total[i];
-    }
-    equal += all;
-    const bool stays = n < length && (!in || (ranked && (key > prefix || (eq && before + (uint32_t)__popcll(eqs & ((1ull << lane) - 1)) < need))));
-    const unsigned long long st = __ballot(stays);
-    __syncthreads();
-    if (lane == 0) total[wave] = (uint32_t)__popcll(st);
-    __syncthreads();
-    before = placed;
-    all = 0;
-    for (int i = 0; i < kSelect / 64; i++) {
-      before += i < wave ? total[i] : 0u;
-      all += total[i];
-    }
-    placed += all;
-    if (stays) {
-      const uint32_t to = before + (uint32_t)__popcll(st & ((1ull << lane) - 1));
-      kept[to] = n;
-      w_out[to] = x;
-    }
-  }
-  for (int i = keep + tid; i < to_capacity; i += kSelect) w_out[i] = 0.f;
+  if ((rest >> lane) & 1) atomicAdd(&hist[digit], 1u);
 }
 
-// One workgroup per block of the new cache, head, and keys or values.
-template <int CODE>
-__global__ __launch_bounds__(kMove) void kv_move_kernel(ns_kv_cache from, ns_kv_cache to, const int32_t *lengths, const int32_t *kept, int keep) {
+struct Choice { uint32_t digit, need, above; };   // the digit, how many of its keys are needed, how many keys lie above it
+
+// The digit that the need-th largest key has, need >= 1; thread t brings the counts of the digits 2 t and 2 t + 1.  All threads call.
+__device__ __forceinline__ Choice choose(uint32_t n0, uint32_t n1, uint32_t need, int tid, uint32_t *shared /* [kWaves + 3] */) {
+  const int lane = tid & 63, wave = tid >> 6;
+  uint32_t from = n0 + n1;                        // of this lane's digits and those above, in the wave
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t x = (uint32_t)__shfl_down((int)from, o);
+    from += lane + o < 64 ? x : 0u;
+  }
+  if (lane == 0) shared[wave] = from;
+  __syncthreads();
+  uint32_t above = from - n0 - n1;
+  for (int w = wave + 1; w < kWaves; w++) above += shared[w];
+  if (above < need && need <= above + n1) {
+    shared[kWaves] = 2 * tid + 1; shared[kWaves + 1] = need - above; shared[kWaves + 2] = above;
+  } else if (above + n1 < need && need <= above + n1 + n0) {
+    shared[kWaves] = 2 * tid; shared[kWaves + 1] = need - above - n1; shared[kWaves + 2] = above + n1;
+  }
+  __syncthreads();
+  const Choice c{shared[kWaves], shared[kWaves + 1], shared[kWaves + 2]};
+  __syncthreads();
+  return c;
+}
+
+struct SelectArgs {
+  const float *weights;
+  const int32_t *lengths;
+  int capacity, keep, n_global, n_recent, heads_kv, to_capacity;
+  int32_t *kept;
+  float *w_out;
+  int32_t *lengths_out;
+};
+
+// A sequence that stays whole; true if it is one.  part of parts: which share of the outputs.
+__device__ __forceinline__ bool all_stay(const SelectArgs &a, int64_t row, int length, int part, int parts, int tid) {
+  if (length > a.keep) {
+    for (int i = a.keep + part * kSelect + tid; i < a.to_capacity; i += parts * kSelect) a.w_out[row * a.to_capacity + i] = 0.f;
+    return false;
+  }
+  for (int i = part * kSelect + tid; i < a.to_capacity; i += parts * kSelect) {
+    if (i < a.keep) a.kept[row * a.keep + i] = i < length ? i : -1;
+    a.w_out[row * a.to_capacity + i] = i < length ? a.weights[row * a.capacity + i] : 0.f;
+  }
+  return true;
+}
+
+// Writes the tokens that stay of KPT * 1024 tokens from `base`: thread's token i is base + wave * 64 KPT + 64 i + lane.  placed, equal: how
+// many stay, and how many have the border's key, before these.
+template <int KPT>
+__device__ __forceinline__ void place(const SelectArgs &a, int64_t row, const float *w, const uint32_t (&key)[KPT], int base, int length,
+                                      uint32_t border, uint32_t need, bool ranked, uint32_t placed, uint32_t equal, int tid, uint32_t *shared /* [2 kWaves] */) {
+  const int lane = tid & 63, wave = tid >> 6;
+  const int first = a.n_global, last = length - a.n_recent;
+  const unsigned long long below = (1ull << lane) - 1;
+  const int n0 = base + wave * 64 * KPT + lane;
+  uint32_t sure = 0, eqs = 0;                     // of the wave: tokens that stay in any case, and with the border's key
+#pragma unroll
+  for (int i = 0; i < KPT; i++) {
+    const int n = n0 + 64 * i;
+    const bool in = n >= first && n < last;
+    sure += (uint32_t)__popcll(__ballot(n < length && (!in || (ranked && key[i] > border))));
+    eqs += (uint32_t)__popcll(__ballot(in && ranked && key[i] == border));
+  }
+  if (lane == 0) {
+    shared[wave] = sure;
+    shared[kWaves + wave] = eqs;
+  }
+  __syncthreads();
+  uint32_t sure_before = 0;
+  for (int x = 0; x < wave; x++) {
+    sure_before += shared[x];
+    equal += shared[kWaves + x];
+  }
+  // all tokens before this wave that stay: the sure ones, and of those with the border's key the first `need`
+  uint32_t at = placed + sure_before, eq = equal;
+#pragma unroll
+  for (int i = 0; i < KPT; i++) {
+    const int n = n0 + 64 * i;
+    const bool in = n >= first && n < last;
+    const bool is_sure = n < length && (!in || (ranked && key[i] > border)), is_eq = in && ranked && key[i] == border;
+    const unsigned long long s = __ballot(is_sure), e = __ballot(is_eq);
+    const uint32_t eq_here = eq + (uint32_t)__popcll(e & below);
+    if (is_sure || (is_eq && eq_here < need)) {
+      const uint32_t to = at + (uint32_t)__popcll(s & below) + min(eq_here, need);
+      a.kept[row * a.keep + to] = n;
+      a.w_out[row * a.to_capacity + to] = w[n];
+    }
+    at += (uint32_t)__popcll(s);
+    eq += (uint32_t)__popcll(e);
+  }
+}
+
+template <int KPT>
+__global__ __launch_bounds__(kSelect) void kv_select_kernel(SelectArgs a) {
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int length = kv_length(a.lengths, b, a.capacity);
+  const int64_t row = (int64_t)b * a.heads_kv + h;
+  if (h == 0 && tid == 0) a.lengths_out[b] = min(length, a.keep);
+  if (all_stay(a, row, length, 0, 1, tid)) return;
+  const float *w = a.weights + row * a.capacity;
+  __shared__ __attribute__((aligned(8))) uint32_t hist[kBins];
+  __shared__ uint32_t shared[2 * kWaves + 3];
+  const int first = a.n_global, last = length - a.n_recent;
+  uint32_t key[KPT];
+#pragma unroll
+  for (int i = 0; i < KPT; i++) {
+    const int n = wave * 64 * KPT + 64 * i + lane;
+    key[i] = n < length ? rank_key(w[n]) : 0u;
+  }
+  uint32_t prefix = 0, need = (uint32_t)(a.keep - a.n_global - a.n_recent);
+  const bool ranked = need > 0;
+  if (ranked) {
+#pragma unroll
+    for (int pass = 0; pass < 3; pass++) {
+      *reinterpret_cast<u32x2 *>(&hist[2 * tid]) = u32x2{0, 0};
+      __syncthreads();
+      const uint32_t mask = pass == 0 ? 0u : ~0u << kShift[pass - 1];
+#pragma unroll
+      for (int i = 0; i < KPT; i++) {
+        const int n = wave * 64 * KPT + 64 * i + lane;
+        count_digits(hist, n >= first && n < last && (key[i] & mask) == prefix, digit_of(key[i], pass), lane);
+      }
+      __syncthreads();
+      const u32x2 counts = *reinterpret_cast<const u32x2 *>(&hist[2 * tid]);
+      const Choice c = choose(counts[0], counts[1], need, tid, shared);
+      prefix |= c.digit << kShift[pass];
+      need = c.need;
+    }
+  }
+  place<KPT>(a, row, w, key, 0, length, prefix, need, ranked, 0, 0, tid, shared);
+}
+
+// ---- longer caches.  Scratch of a sequence and head: a histogram for every digit and chunk, the border's digits so far, and how many of each
+// chunk's keys lie above them.
+struct Scratch {
+  uint32_t *hist;       // [3][chunks][kBins]
+  uint32_t *border;     // [3][2]: after the digit: the key's digits, and how many of its keys are needed
+  uint32_t *above;      // [2][chunks]: keys above the first digit; those that share it above the second
+};
+inline __host__ __device__ size_t scratch_words(int chunks) { return (size_t)3 * chunks * kBins + 8 + 2 * (size_t)chunks; }
+__device__ __forceinline__ Scratch scratch_of(uint32_t *ws, int64_t row, int chunks) {
+  uint32_t *p = ws + row * scratch_words(chunks);
+  return Scratch{p, p + (size_t)3 * chunks * kBins, p + (size_t)3 * chunks * kBins + 8};
+}
+
+// Sum over the workgroup
+__device__ __forceinline__ uint32_t group_sum(uint32_t x, int tid, uint32_t *shared /* [kWaves] */) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += (uint32_t)__shfl_xor((int)x, o);
+  if ((tid & 63) == 0) shared[tid >> 6] = x;
+  __syncthreads();
+  uint32_t sum = 0;
+  for (int w = 0; w < kWaves; w++) sum += shared[w];
+  __syncthreads();
+  return sum;
+}
+
+// The border after digit `pass`, from all chunks' histograms; the first workgroup leaves it for the next launch.  mine: how many of this
+// chunk's keys lie above it.
+__device__ __forceinline__ void border_after(const Scratch &s, int pass, int chunks, int chunk, uint32_t need0, int tid, uint32_t *shared, uint32_t &prefix,
+                                             uint32_t &need, uint32_t &mine) {
+  prefix = pass ? s.border[2 * (pass - 1)] : 0u;
+  need = pass ? s.border[2 * (pass - 1) + 1] : need0;
+  const uint32_t *hist = s.hist + (size_t)pass * chunks * kBins;
+  u32x2 sum = {0, 0}, own = {0, 0};
+  for (int x = 0; x < chunks; x++) {
+    const u32x2 n = *reinterpret_cast<const u32x2 *>(hist + (size_t)x * kBins + 2 * tid);
+    sum += n;
+    if (x == chunk) own = n;
+  }
+  const Choice c = choose(sum[0], sum[1], need, tid, shared);
+  prefix |= c.digit << kShift[pass];
+  need = c.need;
+  if (chunk == 0 && tid == 0) {
+    s.border[2 * pass] = prefix;
+    s.border[2 * pass + 1] = need;
+  }
+  mine = group_sum((2u * tid > c.digit ? own[0] : 0u) + (2u * tid + 1 > c.digit ? own[1] : 0u), tid, shared);
+}
+
+template <int PASS>
+__global__ __launch_bounds__(kSelect) void kv_digit_kernel(SelectArgs a, uint32_t *ws) {
+  const int chunk = blockIdx.x, chunks = gridDim.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int length = kv_length(a.lengths, b, a.capacity);
+  const uint32_t need0 = (uint32_t)(a.keep - a.n_global - a.n_recent);
+  if (length <= a.keep || need0 == 0) return;
+  const int64_t row = (int64_t)b * a.heads_kv + h;
+  const Scratch s = scratch_of(ws, row, chunks);
+  const float *w = a.weights + row * a.capacity;
+  __shared__ __attribute__((aligned(8))) uint32_t hist[kBins];
+  __shared__ uint32_t shared[kWaves + 3];
+  const int first = a.n_global, last = length - a.n_recent, n0 = chunk * kChunk + wave * 64 * kChunkKeys + lane;
+  uint32_t key[kChunkKeys];
+#pragma unroll
+  for (int i = 0; i < kChunkKeys; i++) key[i] = n0 + 64 * i < length ? rank_key(w[n0 + 64 * i]) : 0u;
+  *reinterpret_cast<u32x2 *>(&hist[2 * tid]) = u32x2{0, 0};
+  uint32_t prefix = 0;
+  if (PASS > 0) {
+    uint32_t need, mine;
+    border_after(s, PASS - 1, chunks, chunk, need0, tid, shared, prefix, need, mine);
+    if (tid == 0) s.above[(PASS - 1) * chunks + chunk] = mine;
+  }
+  __syncthreads();
+  const uint32_t mask = PASS == 0 ? 0u : ~0u << kShift[PASS > 0 ? PASS - 1 : 0];
+#pragma unroll
+  for (int i = 0; i < kChunkKeys; i++)
+    count_digits(hist, n0 + 64 * i >= first && n0 + 64 * i < last && (key[i] & mask) == prefix, digit_of(key[i], PASS), lane);
+  __syncthreads();
+  *reinterpret_cast<u32x2 *>(s.hist + ((size_t)PASS * chunks + chunk) * kBins + 2 * tid) = *reinterpret_cast<const u32x2 *>(&hist[2 * tid]);
+}
+
+__global__ __launch_bounds__(kSelect) void kv_place_kernel(SelectArgs a, uint32_t *ws) {
+  const int chunk = blockIdx.x, chunks = gridDim.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int length = kv_length(a.lengths, b, a.capacity);
+  const int64_t row = (int64_t)b * a.heads_kv + h;
+  if (h == 0 && chunk == 0 && tid == 0) a.lengths_out[b] = min(length, a.keep);
+  if (all_stay(a, row, length, chunk, chunks, tid)) return;
+  const float *w = a.weights + row * a.capacity;
+  const uint32_t need0 = (uint32_t)(a.keep - a.n_global - a.n_recent);
+  const bool ranked = need0 > 0;
+  __shared__ uint32_t shared[2 * kWaves + 3];
+  const int first = a.n_global, last = length - a.n_recent, lo = chunk * kChunk;
+  if (lo >= length) return;
+  uint32_t prefix = 0, need = 0, placed = 0, equal = 0;
+  if (ranked) {
+    const Scratch s = scratch_of(ws, row, chunks);
+    uint32_t mine;
+    border_after(s, 2, chunks, chunk, need0, tid, shared, prefix, need, mine);
+    // in the chunks before: keys above the border, and equal to it
+    const uint32_t *hist = s.hist + (size_t)2 * chunks * kBins;
+    const uint32_t digit = digit_of(prefix, 2);
+    for (int x = 0; x < chunk; x++) {
+      const u32x2 n = *reinterpret_cast<const u32x2 *>(hist + (size_t)x * kBins + 2 * tid);
+      placed += (2u * tid > digit ? n[0] : 0u) + (2u * tid + 1 > digit ? n[1] : 0u);
+      if (tid == 0) {
+        placed += s.above[x] + s.above[chunks + x];
+        equal += hist[(size_t)x * kBins + digit];
+      }
+    }
+    placed = group_sum(placed, tid, shared);
+    equal = group_sum(equal, tid, shared);
+  }
+  placed += (uint32_t)(min(lo, first) + max(0, min(lo, length) - max(last, 0)));      // and those that stay in any case
+  const int n0 = lo + wave * 64 * kChunkKeys + lane;
+  uint32_t key[kChunkKeys];
+#pragma unroll
+  for (int i = 0; i < kChunkKeys; i++) key[i] = n0 + 64 * i < length ? rank_key(w[n0 + 64 * i]) : 0u;
+  // (place() counts tokens with the border's key from `equal` on; those of them before that stay are the first `need`)
+  place<kChunkKeys>(a, row, w, key, lo, length, prefix, need, ranked, placed, equal, tid, shared);
+}
+
+// ---- the move
+
+// One workgroup per block of the new cache, head, and keys or values; a thread has up to PIECES times 16 codes.
+template <int CODE, int PIECES, int THREADS>
+__global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_kv_cache to, const int32_t *lengths, const int32_t *kept, int keep) {
   const int b = blockIdx.z, h = blockIdx.y >> 1, value = blockIdx.y & 1, tid = threadIdx.x, block = blockIdx.x;
-  const int lo = block * to.block, hi = min(lo + to.block, min(kv_length(lengths, b, from.capacity), keep));
-  if (lo >= hi) return;
+  const int lo = block * to.block, here = min(to.block, min(kv_length(lengths, b, from.capacity), keep) - lo);
+  if (here <= 0) return;
   const int64_t row = (int64_t)b * to.heads_kv + h;
-  const int quads = to.head_dim / 4, d = tid % quads * 4, step = kMove / quads;
+  const int pieces = to.head_dim / 16, token = tid / pieces, step = THREADS / pieces;      // pieces of a token; tokens between a thread's
+  const int d = tid % pieces * 16, lblock = 31 - __clz(from.block);
   const uint8_t *src = static_cast<const uint8_t *>(value ? from.v : from.k) + b * from.stride_b + h * from.stride_h + d;
   const float *src_scale = (value ? from.v_scale : from.k_scale) + row * (from.capacity / from.block);
   uint8_t *dst = static_cast<uint8_t *>(value ? to.v : to.k) + b * to.stride_b + h * to.stride_h + d;
-  kept += row * keep;
-  uint32_t most = 0;
-  for (int i = lo + tid / quads; i < hi; i += step) {
-    const int n = kept[i];
-    const f32x4 x = kv_decode4<CODE>(*reinterpret_cast<const uint32_t *>(src + n * from.stride_t)) * src_scale[n / from.block];
+  kept += row * keep + lo;
+  u32x4 codes[PIECES];
+  float scale[PIECES], most = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; j++) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+  for (int i = 0; i < PIECES; i++) {
+    const int t = token + i * step;
+    codes[i] = u32x4{0, 0, 0, 0};
+    scale[i] = 0.f;
+    if (t < here) {
+      const int n = kept[t];
+      codes[i] = *reinterpret_cast<const u32x4 *>(src + n * from.stride_t);
+      scale[i] = src_scale[n >> lblock];
+    }
   }
-  __shared__ uint32_t largest[kMove / 64];
+  bool nan = false;
 #pragma unroll
-  for (int o = 32; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  for (int i = 0; i < PIECES; i++) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const f32x4 c = kv_decode4<CODE>(codes[i][j]);
+      top = fmaxf(fmaxf(top, fmaxf(__builtin_fabsf(c[0]), __builtin_fabsf(c[1]))), fmaxf(__builtin_fabsf(c[2]), __builtin_fabsf(c[3])));
+    }
+    nan |= kv_is_nan(scale[i]);
+    most = fmaxf(most, top * scale[i]);
+  }
+  __shared__ float largest[THREADS / 64];
+  if (nan) most = INFINITY;
+  most = wave_max(most);
   if (tid % 64 == 0) largest[tid / 64] = most;
   __syncthreads();
-  most = max(max(largest[0], largest[1]), max(largest[2], largest[3]));
-  const float s = kv_scale_for<CODE>(most);
-  for (int i = lo + tid / quads; i < lo + to.block; i += step) {
-    uint32_t w = 0;
-    if (i < hi && !kv_is_nan(s)) {
-      const int n = kept[i];
-      w = kv_encode4<CODE>(kv_decode4<CODE>(*reinterpret_cast<const uint32_t *>(src + n * from.stride_t)) * src_scale[n / from.block] / s);
+#pragma unroll
+  for (int x = 0; x < THREADS / 64; x++) most = fmaxf(most, largest[x]);
+  const float s = kv_scale_for<CODE>(__float_as_uint(most));
+#pragma unroll
+  for (int i = 0; i < PIECES; i++) {
+    const int t = token + i * step;
+    if (t >= to.block) continue;
+    u32x4 w = codes[i];
+    // (most tokens come from blocks of the same scale: their codes stay as they are)
+    if (scale[i] != s && t < here) {
+      const float ratio = scale[i] / s;               // (exact: s is a power of two)
+#pragma unroll
+      for (int j = 0; j < 4; j++) w[j] = kv_is_nan(s) ? 0u : kv_encode4<CODE>(kv_decode4<CODE>(w[j]) * ratio);
     }
-    *reinterpret_cast<uint32_t *>(dst + i * to.stride_t) = w;
+    *reinterpret_cast<u32x4 *>(dst + (int64_t)(lo + t) * to.stride_t) = w;
   }
   if (tid == 0) (value ? to.v_scale : to.k_scale)[row * (to.capacity / to.block) + block] = s;
 }
 
+int chunks_of(int capacity) { return (capacity + kChunk - 1) / kChunk; }
+
+template <int CODE> void move(const dim3 &grid, hipStream_t s, const ns_kv_cache &from, const ns_kv_cache &to, const int32_t *lengths, const int32_t *kept, int keep) {
+  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, from, to, lengths, kept, keep); };
+  switch (to.block * to.head_dim / 4096) {
+    case 0: case 1: return go(kv_move_kernel<CODE, 1, 256>, 256);
+    case 2: return go(kv_move_kernel<CODE, 2, 256>, 256);
+    case 4: return go(kv_move_kernel<CODE, 4, 256>, 256);
+    default: return go(kv_move_kernel<CODE, 4, 512>, 512);
+  }
+}
+
 }  // namespace
 
-size_t kv_evict_workspace_bytes(const ns_kv_cache &, int) { return 0; }
+size_t kv_evict_workspace_bytes(const ns_kv_cache &from, int) {
+  return from.capacity <= kHeld ? 0 : align_up((size_t)from.batch * from.heads_kv * scratch_words(chunks_of(from.capacity)) * 4, 256);
+}
 
 ns_status launch_kv_evict(const ns_kv_cache &from, const ns_kv_cache &to, const float *weights, const int32_t *lengths, int keep,
-                          int n_global, int n_recent, int32_t *kept, float *w_out, int32_t *lengths_out, void *, hipStream_t s) {
-  hipLaunchKernelGGL(kv_select_kernel, dim3((unsigned)from.heads_kv, (unsigned)from.batch), dim3(kSelect), 0, s, weights, lengths, from.capacity,
-                     keep, n_global, n_recent, from.heads_kv, to.capacity, kept, w_out, lengths_out);
-  const ns_status st = check_launch("kv_select_kernel");
+                          int n_global, int n_recent, int32_t *kept, float *w_out, int32_t *lengths_out, void *ws, hipStream_t s) {
+  const SelectArgs a{weights, lengths, from.capacity, keep, n_global, n_recent, from.heads_kv, to.capacity, kept, w_out, lengths_out};
+  ns_status st;
+  if (from.capacity <= kHeld) {
+    const dim3 grid((unsigned)from.heads_kv, (unsigned)from.batch);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelect), 0, s, a); };
+    from.capacity <= 2 * kSelect ? go(kv_select_kernel<2>) : from.capacity <= 8 * kSelect ? go(kv_select_kernel<8>) : go(kv_select_kernel<32>);
+    st = check_launch("kv_select_kernel");
+  } else {
+    const dim3 grid((unsigned)chunks_of(from.capacity), (unsigned)from.heads_kv, (unsigned)from.batch);
+    uint32_t *p = static_cast<uint32_t *>(ws);
+    hipLaunchKernelGGL(kv_digit_kernel<0>, grid, dim3(kSelect), 0, s, a, p);
+    hipLaunchKernelGGL(kv_digit_kernel<1>, grid, dim3(kSelect), 0, s, a, p);
+    hipLaunchKernelGGL(kv_digit_kernel<2>, grid, dim3(kSelect), 0, s, a, p);
+    hipLaunchKernelGGL(kv_place_kernel, grid, dim3(kSelect), 0, s, a, p);
+    st = check_launch("kv_digit_kernel / kv_place_kernel");
+  }
   if (st != NS_OK) return st;
   const dim3 grid((unsigned)((keep + to.block - 1) / to.block), (unsigned)to.heads_kv * 2, (unsigned)to.batch);
-  if (to.code == NS_CODE_I8)
-    hipLaunchKernelGGL(kv_move_kernel<NS_CODE_I8>, grid, dim3(kMove), 0, s, from, to, lengths, kept, keep);
-  else
-    hipLaunchKernelGGL(kv_move_kernel<NS_CODE_E4M3>, grid, dim3(kMove), 0, s, from, to, lengths, kept, keep);
+  to.code == NS_CODE_I8 ? move<NS_CODE_I8>(grid, s, from, to, lengths, kept, keep) : move<NS_CODE_E4M3>(grid, s, from, to, lengths, kept, keep);
   return check_launch("kv_move_kernel");
 }
 
