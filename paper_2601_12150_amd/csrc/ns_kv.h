@@ -37,25 +37,29 @@ __device__ __forceinline__ int kv_count(const int32_t *counts, int b, int tokens
 }
 
 // ---- codes.  CODE: ns_kv_code
-// the four values of a dword of codes
+// the four values of a dword of codes (int8: bytes c + 128 have a conversion of their own)
 template <int CODE>
 __device__ __forceinline__ f32x4 kv_decode4(uint32_t w) {
-  if (CODE == NS_CODE_I8)
-    return f32x4{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
+  if (CODE == NS_CODE_I8) {
+    const uint32_t u = w ^ 0x80808080u;
+    return f32x4{(float)(u & 0xffu) - 128.f, (float)((u >> 8) & 0xffu) - 128.f, (float)((u >> 16) & 0xffu) - 128.f, (float)(u >> 24) - 128.f};
+  }
   return f32x4{__builtin_amdgcn_cvt_f32_fp8((int)w, 0), __builtin_amdgcn_cvt_f32_fp8((int)w, 1),
                __builtin_amdgcn_cvt_f32_fp8((int)w, 2), __builtin_amdgcn_cvt_f32_fp8((int)w, 3)};
 }
-// the nearest codes (ties to even) of values within the codes' range
+// The nearest codes (ties to even) of x * f, which the codes' range holds.  int8: added to 1.5 2^23 in the multiplication itself, whose one
+// rounding is then the one to a whole number, in two's complement in the low byte.
 template <int CODE>
-__device__ __forceinline__ uint32_t kv_encode4(f32x4 y) {
+__device__ __forceinline__ uint32_t kv_encode4(f32x4 x, float f) {
   if (CODE == NS_CODE_I8) {
-    uint32_t w = 0;
+    uint32_t y[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) w |= ((uint32_t)(int)__builtin_rintf(y[i]) & 0xffu) << (8 * i);
-    return w;
+    for (int i = 0; i < 4; i++) y[i] = __float_as_uint(__builtin_fmaf(x[i], f, 12582912.f));
+    const uint32_t lo = __builtin_amdgcn_perm(y[1], y[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(y[3], y[2], 0x04000c0cu);
+    return lo | hi;
   }
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, w, true);
 }
 
 template <int CODE> __device__ __forceinline__ constexpr float kv_limit() { return CODE == NS_CODE_I8 ? 127.f : 448.f; }   // the largest code
@@ -70,6 +74,8 @@ __device__ __forceinline__ float kv_scale_for(uint32_t most) {
   const int e = CODE == NS_CODE_I8 ? x - 6 + (f > 0x7e0000) : x - 8 + (f > 0x600000);
   return __uint_as_float((uint32_t)(max(e, -100) + 127) << 23);
 }
+// a power of two (whose reciprocal is one too)
+__device__ __forceinline__ bool kv_is_pow2(float s) { return (__float_as_uint(s) & 0x7fffffu) == 0; }
 __device__ __forceinline__ bool kv_is_nan(float s) { return !(s == s); }
 
 // ---- matrix products over codes

@@ -7,50 +7,61 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T> struct Row4;      // four consecutive elements
-template <> struct Row4<float> {
-  static __device__ __forceinline__ f32x4 load(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
-  static __device__ __forceinline__ void store(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+template <typename T> struct Row8;      // eight consecutive elements as they lie in memory
+template <> struct Row8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float *p) { a = reinterpret_cast<const f32x4 *>(p)[0]; b = reinterpret_cast<const f32x4 *>(p)[1]; }
+  __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ f32x4 half(int i) const { return i ? b : a; }
 };
-template <> struct Row4<bf16_t> {
-  static __device__ __forceinline__ f32x4 load(const bf16_t *p) {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
-    return f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
-  }
-  static __device__ __forceinline__ void store(bf16_t *p, f32x4 v) {
-    *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-  }
+template <> struct Row8<bf16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const u32x4 *>(p); }
+  __device__ __forceinline__ void zero() { w = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ f32x4 half(int i) const { return f32x4{bf16_lo(w[2 * i]), bf16_hi(w[2 * i]), bf16_lo(w[2 * i + 1]), bf16_hi(w[2 * i + 1])}; }
 };
+__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // One workgroup per block of tokens that a sequence's new tokens may touch, head, and keys or values.  The scale needs the
-// largest magnitude of all new values of the block, so they are read twice; the second time they come from the L2.
-template <typename T, int CODE>
+// largest magnitude of all new values of the block: a thread has its up to PIECES times 8 in registers until it is known.
+template <typename T, int CODE, int PIECES>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int tokens, const T *k, const T *v, int64_t sb, int64_t sh,
                                                              int64_t st, const int32_t *start, const int32_t *counts) {
   const int b = blockIdx.z, h = blockIdx.y >> 1, value = blockIdx.y & 1, tid = threadIdx.x;
   const int from = kv_length(start, b, c.capacity), to = min(from + kv_count(counts, b, tokens), c.capacity);
-  const int block = from / c.block + (int)blockIdx.x;
-  const int lo = max(from, block * c.block), hi = min(to, (block + 1) * c.block);
+  const int lblock = 31 - __clz(c.block), block = (from >> lblock) + (int)blockIdx.x, begin = block << lblock;
+  const int lo = max(from, begin), hi = min(to, begin + c.block);
   if (lo >= hi) return;
-  const int quads = c.head_dim / 4;                                    // a power of two: 16, 32 or 64
   const T *x = (value ? v : k) + b * sb + h * sh;
   uint8_t *codes = static_cast<uint8_t *>(value ? c.v : c.k) + b * c.stride_b + h * c.stride_h;
-  float *scale = (value ? c.v_scale : c.k_scale) + ((int64_t)b * c.heads_kv + h) * (c.capacity / c.block) + block;
-  const int d = tid % quads * 4, step = kThreads / quads;
+  float *scale = (value ? c.v_scale : c.k_scale) + ((int64_t)b * c.heads_kv + h) * (c.capacity >> lblock) + block;
+  const bool live = from > begin;                                      // tokens before the new ones are in this block
+  const float old = live ? *scale : 0.f;
+  const int lpieces = 31 - __clz(c.head_dim / 8), step = kThreads >> lpieces;      // pieces of a token; tokens between a thread's
+  const int n0 = lo + (tid >> lpieces), d = (tid & ((1 << lpieces) - 1)) * 8;
 
-  uint32_t most = 0;                                                   // magnitudes order like their bits; NaN above all
-  for (int n = lo + tid / quads; n < hi; n += step) {
-    const f32x4 y = Row4<T>::load(x + (int64_t)(n - from) * st + d);
-    most = max(max(most, max(abs_bits(y[0]), abs_bits(y[1]))), max(abs_bits(y[2]), abs_bits(y[3])));
+  Row8<T> y[PIECES];
+#pragma unroll
+  for (int i = 0; i < PIECES; i++) {
+    const int n = n0 + i * step;
+    y[i].zero();
+    if (n < hi) y[i].load(x + (int64_t)(n - from) * st + d);
   }
+  uint32_t most = 0;                                                   // magnitudes order like their bits; NaN above all
+#pragma unroll
+  for (int i = 0; i < PIECES; i++)
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      const f32x4 z = y[i].half(j);
+      most = max(max(most, max(abs_bits(z[0]), abs_bits(z[1]))), max(abs_bits(z[2]), abs_bits(z[3])));
+    }
   __shared__ uint32_t largest[kThreads / 64];
 #pragma unroll
   for (int o = 32; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
   if (tid % 64 == 0) largest[tid / 64] = most;
-  const bool live = from > block * c.block;                            // tokens before the new ones are in this block
-  const float old = live ? *scale : 0.f;
   __syncthreads();
   most = max(max(largest[0], largest[1]), max(largest[2], largest[3]));
   float s = kv_scale_for<CODE>(most);
@@ -58,14 +69,27 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int 
   if (live && (kv_is_nan(old) || (most < kInfBits && __uint_as_float(most) <= kv_limit<CODE>() * old))) s = old;
   if (live && s > old) {                                               // (not with a NaN: the codes no longer matter)
     const float ratio = old / s;
-    for (int n = block * c.block + tid / quads; n < from; n += step) {
-      uint32_t *w = reinterpret_cast<uint32_t *>(codes + n * c.stride_t + d);
-      *w = kv_encode4<CODE>(kv_decode4<CODE>(*w) * ratio);
+    for (int n = begin + (tid >> lpieces); n < from; n += step) {
+      u32x2 *w = reinterpret_cast<u32x2 *>(codes + n * c.stride_t + d);
+      const u32x2 was = *w;
+      *w = u32x2{kv_encode4<CODE>(kv_decode4<CODE>(was[0]), ratio), kv_encode4<CODE>(kv_decode4<CODE>(was[1]), ratio)};
     }
   }
-  for (int n = lo + tid / quads; n < hi; n += step) {
-    const f32x4 y = Row4<T>::load(x + (int64_t)(n - from) * st + d);
-    *reinterpret_cast<uint32_t *>(codes + n * c.stride_t + d) = kv_is_nan(s) ? 0u : kv_encode4<CODE>(y / s);
+  const bool plain = kv_is_pow2(s);                                    // else one of the caller's own: the quotient is rounded, then the code
+  const float inv = plain ? 1.f / s : 1.f;
+#pragma unroll
+  for (int i = 0; i < PIECES; i++) {
+    const int n = n0 + i * step;
+    if (n < hi) {
+      u32x2 w;
+#pragma unroll
+      for (int j = 0; j < 2; j++) {
+        f32x4 z = y[i].half(j);
+        if (!plain) z /= s;
+        w[j] = kv_is_nan(s) ? 0u : kv_encode4<CODE>(z, inv);
+      }
+      *reinterpret_cast<u32x2 *>(codes + n * c.stride_t + d) = w;
+    }
   }
   if (tid == 0) *scale = s;
 }
@@ -87,7 +111,18 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ns_kv_cache c, const 
     s = (value ? c.v_scale : c.k_scale)[((int64_t)b * c.heads_kv + h) * (c.capacity / c.block) + n / c.block];
   }
 #pragma unroll
-  for (int i = 0; i < 4; i++) Row4<T>::store(out + 4 * i, kv_decode4<CODE>(w[i]) * s);
+  for (int i = 0; i < 4; i++) store4(out + 4 * i, kv_decode4<CODE>(w[i]) * s);
+}
+
+template <typename T, int CODE>
+void append(const dim3 &grid, hipStream_t s, const ns_kv_cache &c, int tokens, const void *k, const void *v, int64_t sb, int64_t sh, int64_t st,
+            const int32_t *start, const int32_t *counts) {
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, c, tokens, static_cast<const T *>(k), static_cast<const T *>(v), sb, sh, st, start, counts);
+  };
+  // what a thread has to hold: the block's values, or all the new ones
+  const int values = (min(c.block, tokens) * c.head_dim + 8 * kThreads - 1) / (8 * kThreads);
+  values <= 1 ? go(kv_append_kernel<T, CODE, 1>) : values <= 4 ? go(kv_append_kernel<T, CODE, 4>) : go(kv_append_kernel<T, CODE, 16>);
 }
 
 }  // namespace
@@ -97,14 +132,12 @@ ns_status launch_kv_append(const ns_kv_cache &c, int tokens, int dtype, const vo
   // the blocks that so many tokens touch where they begin at a block's last position
   const int blocks = min((tokens + c.block - 2) / c.block + 1, c.capacity / c.block);
   const dim3 grid((unsigned)blocks, (unsigned)c.heads_kv * 2, (unsigned)c.batch);
-  auto go = [&](auto kernel, auto *kp, auto *vp) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, c, tokens, kp, vp, sb, sh, st, start, counts); };
-  if (dtype == NS_F32) {
-    const float *kp = static_cast<const float *>(k), *vp = static_cast<const float *>(v);
-    c.code == NS_CODE_I8 ? go(kv_append_kernel<float, NS_CODE_I8>, kp, vp) : go(kv_append_kernel<float, NS_CODE_E4M3>, kp, vp);
-  } else {
-    const bf16_t *kp = static_cast<const bf16_t *>(k), *vp = static_cast<const bf16_t *>(v);
-    c.code == NS_CODE_I8 ? go(kv_append_kernel<bf16_t, NS_CODE_I8>, kp, vp) : go(kv_append_kernel<bf16_t, NS_CODE_E4M3>, kp, vp);
-  }
+  if (dtype == NS_F32)
+    c.code == NS_CODE_I8 ? append<float, NS_CODE_I8>(grid, s, c, tokens, k, v, sb, sh, st, start, counts)
+                         : append<float, NS_CODE_E4M3>(grid, s, c, tokens, k, v, sb, sh, st, start, counts);
+  else
+    c.code == NS_CODE_I8 ? append<bf16_t, NS_CODE_I8>(grid, s, c, tokens, k, v, sb, sh, st, start, counts)
+                         : append<bf16_t, NS_CODE_E4M3>(grid, s, c, tokens, k, v, sb, sh, st, start, counts);
   return check_launch("kv_append_kernel");
 }
 

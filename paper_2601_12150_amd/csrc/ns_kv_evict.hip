@@ -26,21 +26,6 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
 }
 __device__ __forceinline__ uint32_t digit_of(uint32_t key, int pass) { return (key >> kShift[pass]) & ((1u << kBits[pass]) - 1); }
 
-// Counts the wave's digits.  Added-up weights crowd in few bins (most tokens get next to nothing), where one LDS atomic per lane would
-// wait for the others: the first two bins that turn up are counted with one addition each.
-__device__ __forceinline__ void count_digits(uint32_t *hist, bool in, uint32_t digit, int lane) {
-  unsigned long long rest = __ballot(in);
-#pragma unroll 1
-  for (int i = 0; i < 2 && rest; i++) {
-    const int leader = __ffsll((long long)rest) - 1;
-    const uint32_t d = (uint32_t)__builtin_amdgcn_readlane((int)digit, leader);
-    const unsigned long long same = __ballot(in && digit == d) & rest;
-    if (lane == leader) atomicAdd(&hist[d], (uint32_t)__popcll(same));
-    rest &= ~same;
-  }
-  if ((rest >> lane) & 1) atomicAdd(&hist[digit], 1u);
-}
-
 struct Choice { uint32_t digit, need, above; };   // the digit, how many of its keys are needed, how many keys lie above it
 
 // The digit that the need-th largest key has, need >= 1; thread t brings the counts of the digits 2 t and 2 t + 1.  All threads call.
@@ -163,7 +148,7 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(SelectArgs a) {
 #pragma unroll
       for (int i = 0; i < KPT; i++) {
         const int n = wave * 64 * KPT + 64 * i + lane;
-        count_digits(hist, n >= first && n < last && (key[i] & mask) == prefix, digit_of(key[i], pass), lane);
+        if (n >= first && n < last && (key[i] & mask) == prefix) atomicAdd(&hist[digit_of(key[i], pass)], 1u);
       }
       __syncthreads();
       const u32x2 counts = *reinterpret_cast<const u32x2 *>(&hist[2 * tid]);
@@ -188,30 +173,40 @@ __device__ __forceinline__ Scratch scratch_of(uint32_t *ws, int64_t row, int chu
   return Scratch{p, p + (size_t)3 * chunks * kBins, p + (size_t)3 * chunks * kBins + 8};
 }
 
-// Sum over the workgroup
-__device__ __forceinline__ uint32_t group_sum(uint32_t x, int tid, uint32_t *shared /* [kWaves] */) {
+// Sums over the workgroup
+__device__ __forceinline__ u32x2 group_sum(u32x2 x, int tid, uint32_t *shared /* [2 kWaves] */) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) x += (uint32_t)__shfl_xor((int)x, o);
-  if ((tid & 63) == 0) shared[tid >> 6] = x;
+  for (int o = 32; o; o >>= 1) x += u32x2{(uint32_t)__shfl_xor((int)x[0], o), (uint32_t)__shfl_xor((int)x[1], o)};
+  if ((tid & 63) == 0) {
+    shared[tid >> 6] = x[0];
+    shared[kWaves + (tid >> 6)] = x[1];
+  }
   __syncthreads();
-  uint32_t sum = 0;
-  for (int w = 0; w < kWaves; w++) sum += shared[w];
+  u32x2 sum = {0, 0};
+  for (int w = 0; w < kWaves; w++) sum += u32x2{shared[w], shared[kWaves + w]};
   __syncthreads();
   return sum;
 }
 
-// The border after digit `pass`, from all chunks' histograms; the first workgroup leaves it for the next launch.  mine: how many of this
-// chunk's keys lie above it.
+// The border after digit `pass`, from all chunks' histograms; the first workgroup leaves it for the next launch.  own, before: the
+// counts of the thread's digits in this chunk and in those before it.
 __device__ __forceinline__ void border_after(const Scratch &s, int pass, int chunks, int chunk, uint32_t need0, int tid, uint32_t *shared, uint32_t &prefix,
-                                             uint32_t &need, uint32_t &mine) {
+                                             uint32_t &need, u32x2 &own, u32x2 &before) {
   prefix = pass ? s.border[2 * (pass - 1)] : 0u;
   need = pass ? s.border[2 * (pass - 1) + 1] : need0;
-  const uint32_t *hist = s.hist + (size_t)pass * chunks * kBins;
-  u32x2 sum = {0, 0}, own = {0, 0};
-  for (int x = 0; x < chunks; x++) {
-    const u32x2 n = *reinterpret_cast<const u32x2 *>(hist + (size_t)x * kBins + 2 * tid);
-    sum += n;
-    if (x == chunk) own = n;
+  const u32x2 *hist = reinterpret_cast<const u32x2 *>(s.hist + (size_t)pass * chunks * kBins) + tid;
+  u32x2 sum = {0, 0};
+  own = before = u32x2{0, 0};
+  for (int x0 = 0; x0 < chunks; x0 += 8) {        // (eight loads on their way at a time)
+    u32x2 n[8];
+#pragma unroll
+    for (int x = 0; x < 8; x++) n[x] = hist[(size_t)min(x0 + x, chunks - 1) * (kBins / 2)];
+#pragma unroll
+    for (int x = 0; x < 8; x++) {
+      if (x0 + x < chunks) sum += n[x];
+      if (x0 + x < chunk) before += n[x];
+      if (x0 + x == chunk) own = n[x];
+    }
   }
   const Choice c = choose(sum[0], sum[1], need, tid, shared);
   prefix |= c.digit << kShift[pass];
@@ -220,7 +215,6 @@ __device__ __forceinline__ void border_after(const Scratch &s, int pass, int chu
     s.border[2 * pass] = prefix;
     s.border[2 * pass + 1] = need;
   }
-  mine = group_sum((2u * tid > c.digit ? own[0] : 0u) + (2u * tid + 1 > c.digit ? own[1] : 0u), tid, shared);
 }
 
 template <int PASS>
@@ -233,7 +227,7 @@ __global__ __launch_bounds__(kSelect) void kv_digit_kernel(SelectArgs a, uint32_
   const Scratch s = scratch_of(ws, row, chunks);
   const float *w = a.weights + row * a.capacity;
   __shared__ __attribute__((aligned(8))) uint32_t hist[kBins];
-  __shared__ uint32_t shared[kWaves + 3];
+  __shared__ uint32_t shared[2 * kWaves + 3];
   const int first = a.n_global, last = length - a.n_recent, n0 = chunk * kChunk + wave * 64 * kChunkKeys + lane;
   uint32_t key[kChunkKeys];
 #pragma unroll
@@ -241,15 +235,18 @@ __global__ __launch_bounds__(kSelect) void kv_digit_kernel(SelectArgs a, uint32_
   *reinterpret_cast<u32x2 *>(&hist[2 * tid]) = u32x2{0, 0};
   uint32_t prefix = 0;
   if (PASS > 0) {
-    uint32_t need, mine;
-    border_after(s, PASS - 1, chunks, chunk, need0, tid, shared, prefix, need, mine);
-    if (tid == 0) s.above[(PASS - 1) * chunks + chunk] = mine;
+    uint32_t need;
+    u32x2 own, before;
+    border_after(s, PASS - 1, chunks, chunk, need0, tid, shared, prefix, need, own, before);
+    const uint32_t digit = digit_of(prefix, PASS - 1), d0 = 2u * (uint32_t)tid;
+    const u32x2 mine = group_sum(u32x2{(d0 > digit ? own[0] : 0u) + (d0 + 1 > digit ? own[1] : 0u), 0u}, tid, shared);
+    if (tid == 0) s.above[(PASS - 1) * chunks + chunk] = mine[0];
   }
   __syncthreads();
   const uint32_t mask = PASS == 0 ? 0u : ~0u << kShift[PASS > 0 ? PASS - 1 : 0];
 #pragma unroll
   for (int i = 0; i < kChunkKeys; i++)
-    count_digits(hist, n0 + 64 * i >= first && n0 + 64 * i < last && (key[i] & mask) == prefix, digit_of(key[i], PASS), lane);
+    if (n0 + 64 * i >= first && n0 + 64 * i < last && (key[i] & mask) == prefix) atomicAdd(&hist[digit_of(key[i], PASS)], 1u);
   __syncthreads();
   *reinterpret_cast<u32x2 *>(s.hist + ((size_t)PASS * chunks + chunk) * kBins + 2 * tid) = *reinterpret_cast<const u32x2 *>(&hist[2 * tid]);
 }
@@ -267,29 +264,24 @@ __global__ __launch_bounds__(kSelect) void kv_place_kernel(SelectArgs a, uint32_
   const int first = a.n_global, last = length - a.n_recent, lo = chunk * kChunk;
   if (lo >= length) return;
   uint32_t prefix = 0, need = 0, placed = 0, equal = 0;
-  if (ranked) {
-    const Scratch s = scratch_of(ws, row, chunks);
-    uint32_t mine;
-    border_after(s, 2, chunks, chunk, need0, tid, shared, prefix, need, mine);
-    // in the chunks before: keys above the border, and equal to it
-    const uint32_t *hist = s.hist + (size_t)2 * chunks * kBins;
-    const uint32_t digit = digit_of(prefix, 2);
-    for (int x = 0; x < chunk; x++) {
-      const u32x2 n = *reinterpret_cast<const u32x2 *>(hist + (size_t)x * kBins + 2 * tid);
-      placed += (2u * tid > digit ? n[0] : 0u) + (2u * tid + 1 > digit ? n[1] : 0u);
-      if (tid == 0) {
-        placed += s.above[x] + s.above[chunks + x];
-        equal += hist[(size_t)x * kBins + digit];
-      }
-    }
-    placed = group_sum(placed, tid, shared);
-    equal = group_sum(equal, tid, shared);
-  }
-  placed += (uint32_t)(min(lo, first) + max(0, min(lo, length) - max(last, 0)));      // and those that stay in any case
   const int n0 = lo + wave * 64 * kChunkKeys + lane;
   uint32_t key[kChunkKeys];
 #pragma unroll
   for (int i = 0; i < kChunkKeys; i++) key[i] = n0 + 64 * i < length ? rank_key(w[n0 + 64 * i]) : 0u;
+  if (ranked) {
+    const Scratch s = scratch_of(ws, row, chunks);
+    u32x2 own, before;
+    border_after(s, 2, chunks, chunk, need0, tid, shared, prefix, need, own, before);
+    // in the chunks before: keys above the border, and equal to it
+    const uint32_t digit = digit_of(prefix, 2), d0 = 2u * (uint32_t)tid;
+    placed = (d0 > digit ? before[0] : 0u) + (d0 + 1 > digit ? before[1] : 0u);
+    equal = (d0 == digit ? before[0] : 0u) + (d0 + 1 == digit ? before[1] : 0u);
+    for (int x = tid; x < chunk; x += kSelect) placed += s.above[x] + s.above[chunks + x];
+    const u32x2 sums = group_sum(u32x2{placed, equal}, tid, shared);
+    placed = sums[0];
+    equal = sums[1];
+  }
+  placed += (uint32_t)(min(lo, first) + max(0, min(lo, length) - max(last, 0)));      // and those that stay in any case
   // (place() counts tokens with the border's key from `equal` on; those of them before that stay are the first `need`)
   place<kChunkKeys>(a, row, w, key, lo, length, prefix, need, ranked, placed, equal, tid, shared);
 }
@@ -351,7 +343,7 @@ __global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_k
     if (scale[i] != s && t < here) {
       const float ratio = scale[i] / s;               // (exact: s is a power of two)
 #pragma unroll
-      for (int j = 0; j < 4; j++) w[j] = kv_is_nan(s) ? 0u : kv_encode4<CODE>(kv_decode4<CODE>(w[j]) * ratio);
+      for (int j = 0; j < 4; j++) w[j] = kv_is_nan(s) ? 0u : kv_encode4<CODE>(kv_decode4<CODE>(w[j]), ratio);
     }
     *reinterpret_cast<u32x4 *>(dst + (int64_t)(lo + t) * to.stride_t) = w;
   }
@@ -383,7 +375,7 @@ ns_status launch_kv_evict(const ns_kv_cache &from, const ns_kv_cache &to, const 
   if (from.capacity <= kHeld) {
     const dim3 grid((unsigned)from.heads_kv, (unsigned)from.batch);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelect), 0, s, a); };
-    from.capacity <= 2 * kSelect ? go(kv_select_kernel<2>) : from.capacity <= 8 * kSelect ? go(kv_select_kernel<8>) : go(kv_select_kernel<32>);
+    from.capacity <= 2 * kSelect ? go(kv_select_kernel<2>) : from.capacity <= 8 * kSelect ? go(kv_select_kernel<8>) : from.capacity <= 16 * kSelect ? go(kv_select_kernel<16>) : go(kv_select_kernel<32>);
     st = check_launch("kv_select_kernel");
   } else {
     const dim3 grid((unsigned)chunks_of(from.capacity), (unsigned)from.heads_kv, (unsigned)from.batch);
