@@ -150,7 +150,13 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   const uint32_t stride = (uint32_t)c.stride_t;
   u32x4 kraw[KP];
   uint32_t vraw[VP][4];
+  float next_ks[2], next_vs[2], staged_ks[2] = {0.f, 0.f};    // scales of the fetched tile, and K's of the staged one
   auto fetch = [&](int n0) {
+    const int n1 = min(n0 + 32, c.capacity - 32);   // (behind the capacity: masked, any scale will do)
+    next_ks[0] = ks[n0 >> lblock];
+    next_ks[1] = ks[n1 >> lblock];
+    next_vs[0] = vs[n0 >> lblock];
+    next_vs[1] = vs[n1 >> lblock];
     const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
     const int most = c.capacity - 1 - n0;           // (the last tile of blocks of 32 may reach beyond the capacity)
 #pragma unroll
@@ -167,8 +173,9 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   float unit = 0.f, next = 0.f, rel0 = 1.f, rel1 = 1.f;
   bool slow = false;
   auto stage = [&](int n0, uint32_t at) {
-    const int n1 = min(n0 + 32, c.capacity - 32);
-    const float s0 = vs[n0 >> lblock], s1 = n0 + 32 < length ? vs[n1 >> lblock] : s0, big = fmaxf(s0, s1);
+    staged_ks[0] = next_ks[0];
+    staged_ks[1] = next_ks[1];
+    const float s0 = next_vs[0], s1 = n0 + 32 < length ? next_vs[1] : s0, big = fmaxf(s0, s1);
     if (!(big <= next * 0x1p7f) && big > 0.f && big < INFINITY) next = big;      // (the first tile's too)
     rel0 = s0 / next;
     rel1 = s1 / next;
@@ -217,7 +224,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   const uint32_t k_lane = k_at<D>(n32, hh), v_lane = kV + v_at(n32, hh);
   int n0 = n_lo;
   // one tile: its logits, weights and values.  SLOW: its V holds bare codes
-  auto tile_of_keys = [&](auto is_slow, float f_v0, float f_v1, float tile_unit) {
+  auto tile_of_keys = [&](auto is_slow, float f_v0, float f_v1, float tile_unit, float sk0, float sk1) {
     constexpr bool SLOW = decltype(is_slow)::value;
     const bool edge = n0 + kKeys > every;
     const uint32_t kl = (uint32_t)opaque((int)(k_lane + at)), vl = (uint32_t)opaque((int)(v_lane + at));
@@ -237,22 +244,26 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
         if (!EARLY && k % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (not all operands at once)
       }
     }
-    const int n1 = min(n0 + 32, c.capacity - 32);     // (behind the capacity: masked, any scale will do)
-    const float sk[2] = {ks[n0 >> lblock], ks[n1 >> lblock]};
     const bool fresh = m == -INFINITY;
     const float ref = fresh ? 0.f : m;
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 2; x++) {
-      const float f = factor * sk[x];
+      const float f = factor * (x ? sk1 : sk0);
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        float z = __builtin_fmaf(s[x][e], f, -ref);
-        if (edge) z = n0 + x * 32 + (e >> 2) * 8 + hh * 4 + (e & 3) < limit ? z : -INFINITY;
-        s[x][e] = z;
-        top = fmaxf(top, z);
-      }
+      for (int e = 0; e < 16; e++) s[x][e] = __builtin_fmaf(s[x][e], f, -ref);
     }
+    if (edge) {
+      asm volatile("; masked");                       // (a branch, not a select for every logit of every tile)
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[x][e] = n0 + x * 32 + (e >> 2) * 8 + hh * 4 + (e & 3) < limit ? s[x][e] : -INFINITY;
+    }
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) top = fmaxf(top, s[x][e]);
     if (__any(top > kRoom || (fresh && top > -INFINITY)) || tile_unit != unit) {
       top = half_swap_max(top);
       const bool moved = top > kRoom || (fresh && top > -INFINITY);
@@ -270,13 +281,14 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
       for (int i = 0; i < MT; i++) o[i] *= fade;
     }
     Frag pf[PARTS][4];
+    float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 2; x++)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f(s[x][e]), p1 = __builtin_amdgcn_exp2f(s[x][e + 1]);
-        l += p0;
-        l += p1;
+        ls[e % 4] += p0;
+        ls[e % 4 + 1] += p1;
         const uint32_t hi = pack_f16(p0, p1);
         pf[0][x * 2 + e / 8].w[e % 8 / 2] = hi;
         if (PARTS == 2) {
@@ -284,6 +296,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
           pf[PARTS - 1][x * 2 + e / 8].w[e % 8 / 2] = pack_f16(p0 - (float)w[0], p1 - (float)w[1]);
         }
       }
+    l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (!SLOW) {
 #pragma unroll
       for (int i = 0; i < MT; i++)
@@ -342,15 +355,15 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   while (n0 < n_wave) {
     if constexpr (EARLY)
       while (n0 < n_wave && !slow) {
-        const float u = next;
+        const float u = next, k0 = staged_ks[0], k1 = staged_ks[1];
         ahead();
-        tile_of_keys(std::false_type{}, 0.f, 0.f, u);
+        tile_of_keys(std::false_type{}, 0.f, 0.f, u, k0, k1);
         step();
       }
     while (n0 < n_wave && slow) {
-      const float u = next, f0 = rel0, f1 = rel1;
+      const float u = next, f0 = rel0, f1 = rel1, k0 = staged_ks[0], k1 = staged_ks[1];
       ahead();
-      tile_of_keys(std::true_type{}, f0, f1, u);
+      tile_of_keys(std::true_type{}, f0, f1, u, k0, k1);
       step();
     }
   }
