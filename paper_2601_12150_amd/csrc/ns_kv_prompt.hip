@@ -68,9 +68,11 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   const int n32 = lane & 31, hh = lane >> 5;
   const int G = d.heads / c.heads_kv, R = G * d.tokens;
   const int tiles = (R + ROWS - 1) / ROWS;
-  // the last rows see most: they go first
-  const int part = (int)blockIdx.x % (D / DV), x_tile = (int)blockIdx.x / (D / DV);
-  const int tile = tiles - 1 - x_tile / a.splits, split = x_tile % a.splits, h = blockIdx.y, b = blockIdx.z;
+  // The last rows of all heads see most and go first, so that the launch ends with small pieces.  Neighbouring workgroups, which
+  // run on different XCDs, have different heads: with a multiple of eight of them a head's K and V stay in one XCD's L2.
+  const uint32_t heads = (uint32_t)c.batch * c.heads_kv, item = blockIdx.x / heads, head = blockIdx.x % heads;
+  const int part = (int)(item % (D / DV)), split = (int)(item / (D / DV) % a.splits), tile = tiles - 1 - (int)(item / (D / DV) / a.splits);
+  const int h = (int)(head % c.heads_kv), b = (int)(head / c.heads_kv);
   const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
   const int64_t row = (int64_t)b * c.heads_kv + h;
 
@@ -627,7 +629,7 @@ ns_status launch(const KvAttnArgs &a) {
   T *out = static_cast<T *>(a.out);
   ns_status st = reserve_lds_once(reinterpret_cast<const void *>(kv_prompt_kernel<T, CODE, D, DV, WAVES>), lds);
   if (st != NS_OK) return st;
-  const dim3 grid((unsigned)(tiles * w.splits * (D / DV)), (unsigned)c.heads_kv, (unsigned)c.batch);
+  const dim3 grid((unsigned)((int64_t)tiles * w.splits * (D / DV) * c.heads_kv * c.batch));
   hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES>), grid, dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out, a.lse, p);
   st = check_launch("kv_prompt_kernel");
   if (st == NS_OK && w.splits > 1) {
