@@ -99,6 +99,19 @@ template <int CODE, int HALF> __device__ __forceinline__ uint32_t kv_f16x2(uint3
   }
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)raw, 1.f, HALF));
 }
+// The same times f, a power of two that leaves them exact: in the instruction that makes them.  kv_by<CODE>(f) is what the conversion takes.
+template <int CODE> struct By { f16x2 f, bias; float scale; };
+template <int CODE> __device__ __forceinline__ By<CODE> kv_by(float f) {
+  const _Float16 h = (_Float16)f, b = (_Float16)(-1152.f * f);
+  return By<CODE>{f16x2{h, h}, f16x2{b, b}, f};
+}
+template <int CODE, int HALF> __device__ __forceinline__ uint32_t kv_f16x2_by(uint32_t raw, const By<CODE> &by) {
+  if (CODE == NS_CODE_I8) {
+    const uint32_t u = __builtin_amdgcn_perm(0x64646464u, raw, HALF ? 0x07030602u : 0x05010400u);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, u), by.f, by.bias));
+  }
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)raw, by.scale, HALF));
+}
 // eight consecutive codes
 template <int CODE> __device__ __forceinline__ Frag kv_frag(uint32_t lo, uint32_t hi) {
   lo = kv_raw<CODE>(lo);

@@ -42,10 +42,11 @@ template <int D> __device__ __forceinline__ uint32_t k_at(int key, int piece) {
 __device__ __forceinline__ uint32_t v_at(int channel, int piece) {
   return (uint32_t)(channel * kKeys * 2 + ((piece ^ ((channel & 7) ^ ((channel >> 3) & 3))) * 16));
 }
-// 2^x exactly, 2^-10 <= s <= 2^7: what V's codes are multiplied with in fp16 without a rounding (e4m3's least code is 2^-9, of 3 bits)
+// 2^x exactly, 2^-10 <= s <= 2^5: what V's codes are multiplied with in fp16 without a rounding (e4m3's least code is 2^-9; 1152 + 127
+// times it is below 65504)
 __device__ __forceinline__ bool plain_ratio(float s) {
   const uint32_t u = __float_as_uint(s);
-  return (u & 0x7fffffu) == 0 && u >= (117u << 23) && u <= (134u << 23);
+  return (u & 0x7fffffu) == 0 && u >= (117u << 23) && u <= (132u << 23);
 }
 
 // What a launch leaves for the joins and for the weights' pass: records [split][head][row], and the rows' operands.
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   constexpr int KP = kKeys * D / 16 / THREADS, VP = kKeys / 4 * (DV / 4) / THREADS;      // pieces a thread has of K (16 codes) and V (4 x 4)
   constexpr int KR = THREADS / (D / 16), VR = THREADS / (DV / 4) * 4;                    // keys between two of its pieces
   const int k_key = tid / (D / 16), v_key = tid / (DV / 4) * 4;
-  const uint32_t stride = (uint32_t)c.stride_t;
+  const uint32_t stride = (uint32_t)c.stride_t, k_off = (uint32_t)k_key * stride + tid % (D / 16) * 16, v_off = (uint32_t)v_key * stride + tid % (DV / 4) * 4;
   u32x4 kraw[KP];
   uint32_t vraw[VP][4];
   float next_ks[2], next_vs[2], staged_ks[2] = {0.f, 0.f};    // scales of the fetched tile, and K's of the staged one
@@ -160,29 +161,33 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
     next_vs[0] = vs[n0 >> lblock];
     next_vs[1] = vs[n1 >> lblock];
     const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
-    const int most = c.capacity - 1 - n0;           // (the last tile of blocks of 32 may reach beyond the capacity)
+    // (the last tile of blocks of 32 may reach 32 keys beyond the capacity: their places take the 32 before once more)
+    const uint32_t back = n0 + kKeys > c.capacity ? 32 * stride : 0u;
 #pragma unroll
-    for (int i = 0; i < KP; i++) kraw[i] = *reinterpret_cast<const u32x4 *>(kp + ((uint32_t)min(k_key + i * KR, most) * stride + tid % (D / 16) * 16));
+    for (int i = 0; i < KP; i++)
+      kraw[i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)i * KR * c.stride_t + (k_off - (k_key + i * KR >= 32 ? back : 0u)));
 #pragma unroll
     for (int i = 0; i < VP; i++)
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        vraw[i][j] = *reinterpret_cast<const uint32_t *>(vp + ((uint32_t)min(v_key + i * VR + j, most) * stride + tid % (DV / 4) * 4));
+        vraw[i][j] = *reinterpret_cast<const uint32_t *>(vp + (int64_t)(i * VR + j) * c.stride_t + (v_off - (v_key + i * VR >= 32 ? back : 0u)));
   };
   // V's scales: o is in units of `unit`, a tile's V in LDS in units of `next`, which is the same but where a much larger scale
   // comes along.  Where both halves' scales are next times a plain ratio, V is multiplied by that on its way (slow = false); else (a NaN, far
   // smaller ones, the caller's own that are no powers of two) LDS has the bare codes, and the products are multiplied.
-  float unit = 0.f, next = 0.f, rel0 = 1.f, rel1 = 1.f;
+  float unit = 0.f, next = 0.f, inv_next = 0.f, rel0 = 1.f, rel1 = 1.f;
   bool slow = false;
   auto stage = [&](int n0, uint32_t at) {
     staged_ks[0] = next_ks[0];
     staged_ks[1] = next_ks[1];
     const float s0 = next_vs[0], s1 = n0 + 32 < length ? next_vs[1] : s0, big = fmaxf(s0, s1);
-    if (!(big <= next * 0x1p7f) && big > 0.f && big < INFINITY) next = big;      // (the first tile's too)
-    rel0 = s0 / next;
-    rel1 = s1 / next;
+    if (!(big <= next * 0x1p5f) && big > 0.f && big < INFINITY) {                // (the first tile's too)
+      next = big;
+      inv_next = 1.f / big;
+    }
+    rel0 = s0 * inv_next;
+    rel1 = s1 * inv_next;
     slow = !EARLY || !(plain_ratio(rel0) && plain_ratio(rel1));
-    const _Float16 h0 = (_Float16)(slow ? 1.f : rel0), h1 = (_Float16)(slow ? 1.f : rel1);
     // (opaque: else the compiler keeps every address in a register of its own)
     const uint32_t k_to = (uint32_t)opaque((int)(at + k_at<D>(k_key, tid % (D / 16) * 2)));
     const int quad0 = v_key / 4;
@@ -204,14 +209,13 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
       for (int j = 0; j < 4; j++) w[j] = kv_raw<CODE>(tail && n0 + key + j >= length ? 0u : vraw[i][j]);
       const uint32_t lo0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
       const uint32_t hi0 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
-      const _Float16 f = key >= 32 ? h1 : h0;
-      auto times = [&](uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * f16x2{f, f}); };
+      const By<CODE> by = kv_by<CODE>(slow ? 1.f : key >= 32 ? rel1 : rel0);
       // keys 4 quad .. + 3 are the first or second half of the piece that lanes of half (quad & 1) read for the step quad / 4
       const uint32_t to = v_to ^ (uint32_t)(VR * 2 * i);
-      *reinterpret_cast<u32x2 *>(lds + to) = u32x2{times(kv_f16x2<CODE, 0>(lo0)), times(kv_f16x2<CODE, 0>(lo1))};
-      *reinterpret_cast<u32x2 *>(lds + (to ^ 16) + kKeys * 2) = u32x2{times(kv_f16x2<CODE, 1>(lo0)), times(kv_f16x2<CODE, 1>(lo1))};
-      *reinterpret_cast<u32x2 *>(lds + (to ^ 32) + kKeys * 4) = u32x2{times(kv_f16x2<CODE, 0>(hi0)), times(kv_f16x2<CODE, 0>(hi1))};
-      *reinterpret_cast<u32x2 *>(lds + (to ^ 48) + kKeys * 6) = u32x2{times(kv_f16x2<CODE, 1>(hi0)), times(kv_f16x2<CODE, 1>(hi1))};
+      *reinterpret_cast<u32x2 *>(lds + to) = u32x2{kv_f16x2_by<CODE, 0>(lo0, by), kv_f16x2_by<CODE, 0>(lo1, by)};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 16) + kKeys * 2) = u32x2{kv_f16x2_by<CODE, 1>(lo0, by), kv_f16x2_by<CODE, 1>(lo1, by)};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 32) + kKeys * 4) = u32x2{kv_f16x2_by<CODE, 0>(hi0, by), kv_f16x2_by<CODE, 0>(hi1, by)};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 48) + kKeys * 6) = u32x2{kv_f16x2_by<CODE, 1>(hi0, by), kv_f16x2_by<CODE, 1>(hi1, by)};
     }
   };
 
@@ -289,9 +293,9 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f(s[x][e]), p1 = __builtin_amdgcn_exp2f(s[x][e + 1]);
+        const uint32_t hi = pack_f16(p0, p1);
         ls[e % 4] += p0;
         ls[e % 4 + 1] += p1;
-        const uint32_t hi = pack_f16(p0, p1);
         pf[0][x * 2 + e / 8].w[e % 8 / 2] = hi;
         if (PARTS == 2) {
           const f16x2 w = __builtin_bit_cast(f16x2, hi);
