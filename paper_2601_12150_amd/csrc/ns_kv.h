@@ -136,9 +136,79 @@ template <int CODE> __device__ __forceinline__ void kv_frags_t(const uint32_t (&
 // most 2^-39 of the largest.
 __device__ __forceinline__ int kv_row_shift(uint32_t most) { return most >= kInfBits ? 0 : 141 - (int)(most >> 23); }   // q is taken times 2^this
 
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+}
+template <typename T> __device__ __forceinline__ f32x4 load4(const T *p);
+template <> __device__ __forceinline__ f32x4 load4<float>(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+template <> __device__ __forceinline__ f32x4 load4<bf16_t>(const bf16_t *p) {
+  const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+  return f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
+}
+__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
+
+// Weights are 2^(z - m + 11) in fp16, m a logit near the largest so far, which is moved up before they pass 2^15: a weight that is the
+// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.
+constexpr float kLift = 11.f, kRoom = 15.f;
+
 // positions that query t sees: 0 .. limit - 1
 __device__ __forceinline__ int kv_seen(const ns_kv_attn_desc &d, int t, int length, int count) {
   return t >= count ? 0 : d.causal ? max(length - count + t + 1, 0) : length;
 }
+
+// ---- the weights' second pass over K (ns_kv_prompt.hip): its operands, 16 rows of queries r = token * group + head at a time.  Channels of the
+// step s = 2 i + f that lane (n, g) has: 64 i + 16 g + 8 f + j, so that 16 bytes of codes are two operands.  One wave.
+template <typename T>
+__device__ __forceinline__ void kv_rows_tile(const ns_kv_cache &c, const ns_kv_attn_desc &d, const T *q, int b, int h, int tile, int lane, Frag *frags,
+                                             float *factors) {
+  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
+  const int n16 = lane & 15, g = lane >> 4, KS = c.head_dim / 32;
+  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 15) / 16;
+  const int64_t row = (int64_t)b * c.heads_kv + h;
+  const int r = tile * 16 + n16;
+  const bool real = r < R;
+  const int t = real ? r / G : 0;
+  const T *p = q + b * d.q_stride_b + (int64_t)(h * G + (real ? r - t * G : 0)) * d.q_stride_h + (int64_t)t * d.q_stride_t + 16 * g;
+  uint32_t most = 0;
+  for (int i = 0; i < KS / 2; i++)
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const f32x4 x = load4(p + 64 * i + 4 * k);
+#pragma unroll
+      for (int j = 0; j < 4; j++) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
+    }
+  most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+  most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+  const int shift = kv_row_shift(most);
+  if (g == 0) factors[row * tiles * 16 + r] = real ? ldexpf(d.scale * kLog2e, -shift) : 0.f;
+  for (int s = 0; s < KS; s++) {
+    Frag f[PARTS];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      const f32x4 x = load4(p + 64 * (s / 2) + 8 * (s % 2) + 4 * k);
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const float x0 = real ? ldexpf(x[j], shift) : 0.f, x1 = real ? ldexpf(x[j + 1], shift) : 0.f;
+        f[0].w[2 * k + j / 2] = pack_f16(x0, x1);
+        if (PARTS == 2) {
+          const f16x2 w = __builtin_bit_cast(f16x2, f[0].w[2 * k + j / 2]);
+          f[PARTS - 1].w[2 * k + j / 2] = pack_f16(x0 - (float)w[0], x1 - (float)w[1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int pt = 0; pt < PARTS; pt++) frags[(((row * tiles + tile) * PARTS + pt) * KS + s) * 64 + lane] = f[pt];
+  }
+}
+inline size_t kv_rows_padded(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
+  return (size_t)c.batch * c.heads_kv * (((size_t)(d.heads / c.heads_kv) * d.tokens + 15) / 16) * 16;
+}
+inline size_t kv_rows_frag_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
+  return align_up(kv_rows_padded(c, d) * c.head_dim * 2 * (d.dtype == NS_F32 ? 2 : 1), 256);
+}
+inline size_t kv_rows_factor_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return align_up(kv_rows_padded(c, d) * 4, 256); }
+// lse2 [B Hkv][R]: log2 of the rows' sums, +inf for a row that sees nothing; rows: the operands are yet to be made
+ns_status launch_kv_weights_again(const KvAttnArgs &a, Frag *frags, float *factors, const float *lse2, bool rows);
 
 }  // namespace ns

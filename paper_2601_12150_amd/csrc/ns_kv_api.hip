@@ -68,6 +68,7 @@ ns_status validate_attn(const ns_kv_cache *c, const ns_kv_attn_desc *d) {
   if (d->heads % c->heads_kv) return fail(NS_ERR_INVALID_ARG, "heads (%d) must be a multiple of heads_kv (%d)", d->heads, c->heads_kv);
   if (d->heads > 1024) return fail(NS_ERR_UNSUPPORTED, "more than 1024 query heads");
   if ((int64_t)d->heads * d->tokens > (1 << 24)) return fail(NS_ERR_UNSUPPORTED, "heads x tokens above 2^24");
+  if ((int64_t)c->batch * c->heads_kv * ((c->capacity + 127) / 128) > 0x7fffffff) return fail(NS_ERR_UNSUPPORTED, "batch x heads_kv x capacity above 2^38");
   if ((st = validate_dtype(d->dtype)) != NS_OK) return st;
   if (!(d->scale - d->scale == 0.f)) return fail(NS_ERR_INVALID_ARG, "scale must be finite");
   if ((st = validate_rows(d->q_stride_b, d->q_stride_h, d->q_stride_t, d->dtype, c->head_dim, "q")) != NS_OK) return st;

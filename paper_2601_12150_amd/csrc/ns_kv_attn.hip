@@ -10,113 +10,229 @@
 // byte permutations; nothing goes through LDS in the loop.  K's channels are taken in an order that makes a lane's 16 bytes two
 // operands.
 //
-// Every launch has as many workgroups as the chip holds at once, and each takes an equal share of all sequences' tokens
+// A launch has as many workgroups as the chip holds at once, and each takes an equal share of all sequences' tokens
 // (tiles of 128, counted in device memory, so that a recorded graph follows the lengths): partial results of a head that
-// several workgroups share are joined by kv_attn_join_kernel.
+// several workgroups share are joined by kv_attn_join_kernel.  Small caches are not shared out: a workgroup of eight waves per
+// head writes its result itself, in one launch.
+//
+// The weights that positions are given need the rows' sums, which are known at the end: few rows leave their logits (4 bytes a row and
+// key, written and read), more rows have K read again (D bytes a key) by kv_weights_sum_kernel.
 #include "ns_kv.h"
+#include <algorithm>
 
 namespace ns {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kSub = 32, kTile = kWaves * kSub;
-// Weights are 2^(z - m + 11) in fp16, m a logit near the largest so far, which is moved up before they pass 2^15: a weight that is the
-// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.
-constexpr float kLift = 11.f, kRoom = 15.f;
+constexpr int kThreads = 256, kWaves = 4, kSub = 32, kTile = kWaves * kSub, kMostParts = 1024;
 
-struct Span { int64_t lo, hi; };                  // tiles of this workgroup
-
-// Sum over the wave of a small count
-__device__ __forceinline__ int wave_total(int x) {
+// Sums over the lanes up to and including each
+__device__ __forceinline__ int wave_upto(int x, int lane) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    x += lane >= o ? y : 0;
+  }
   return x;
 }
-
 __device__ __forceinline__ int tiles_of(const int32_t *lengths, int b, int batch, int capacity) {
   return b < batch ? (kv_length(lengths, b, capacity) + kTile - 1) / kTile : 0;
 }
 
-// Tiles of all sequences (one head).  The whole wave calls.
-__device__ __forceinline__ int64_t all_tiles(const int32_t *lengths, int batch, int capacity, int lane) {
-  int64_t sum = 0;
-  for (int b = 0; b < batch; b += 64) sum += wave_total(tiles_of(lengths, b + lane, batch, capacity));
-  return sum;
-}
-
-// Where a tile lies: sequence b, whose tiles of all heads begin at `first`, and its number of tiles per head.
-struct Place { int b, tiles; int64_t first; };
-__device__ __forceinline__ Place place_of(const int32_t *lengths, int batch, int capacity, int heads_kv, int64_t tile, int lane) {
-  int64_t first = 0;
-  for (int b = 0; b < batch; b += 64) {
-    const int mine = tiles_of(lengths, b + lane, batch, capacity);
-    int upto = mine;                              // tiles of this lane's sequence and those before
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(upto, o);
-      upto += lane >= o ? x : 0;
-    }
-    const unsigned long long past = __ballot(first + (int64_t)upto * heads_kv > tile);
-    if (past) {
-      const int at = __ffsll((long long)past) - 1, n = __shfl(mine, at);
-      return Place{b + at, n, first + (int64_t)(__shfl(upto, at) - n) * heads_kv};
-    }
-    first += (int64_t)__shfl(upto, 63) * heads_kv;
+// The tiles of all sequences and heads, in the order sequence, head, token, shared out over the workgroups (there are fewer than 2^31;
+// the host sees to that).  The whole wave calls, with uniform arguments.
+struct Tiles {
+  const int32_t *lengths;
+  int batch, capacity, heads_kv, lane;
+  int mine, upto;                                 // of the first 64 sequences: this lane's tiles per head, and with those before
+  __device__ __forceinline__ Tiles(const int32_t *lengths, const ns_kv_cache &c, int lane)
+      : lengths(lengths), batch(c.batch), capacity(c.capacity), heads_kv(c.heads_kv), lane(lane) {
+    mine = tiles_of(lengths, lane, batch, capacity);
+    upto = wave_upto(mine, lane);
   }
-  return Place{batch, 0, first};
+  // ... of a later 64
+  __device__ __forceinline__ void later(int b, int &n, int &to) const {
+    n = tiles_of(lengths, b + lane, batch, capacity);
+    to = wave_upto(n, lane);
+  }
+  __device__ __forceinline__ int all() const {
+    int sum = __builtin_amdgcn_readlane(upto, 63);
+    for (int b = 64; b < batch; b += 64) {
+      int n, to;
+      later(b, n, to);
+      sum += __builtin_amdgcn_readlane(to, 63);
+    }
+    return sum * heads_kv;
+  }
+  // tiles per workgroup
+  __device__ __forceinline__ int share(int workgroups) const { return max((all() + workgroups - 1) / workgroups, 1); }
+  // the tiles of the sequences before b
+  __device__ __forceinline__ int before(int b) const {
+    if (b == 0) return 0;
+    int sum = __builtin_amdgcn_readlane(upto, min(b, 64) - 1);
+    for (int x = 64; x < b; x += 64) {
+      int n, to;
+      later(x, n, to);
+      sum += __builtin_amdgcn_readlane(to, min(b - x, 64) - 1);
+    }
+    return sum * heads_kv;
+  }
+  // where a tile lies: sequence b, whose tiles of all heads begin at `first`, and its number of tiles per head
+  __device__ __forceinline__ void place(int tile, int &b, int &tiles, int &first) const {
+    first = 0;
+    int n = mine, to = upto;
+    for (int x = 0; x < batch; x += 64) {
+      if (x) later(x, n, to);
+      const unsigned long long past = __ballot(first + to * heads_kv > tile);
+      if (past) {
+        const int at = __ffsll((long long)past) - 1;
+        tiles = __builtin_amdgcn_readlane(n, at);
+        first += (__builtin_amdgcn_readlane(to, at) - tiles) * heads_kv;
+        b = x + at;
+        return;
+      }
+      first += __builtin_amdgcn_readlane(to, 63) * heads_kv;
+    }
+    b = 0;                                        // (not reached: the tile is one of them)
+    tiles = 1;
+  }
+};
+
+// What the launches leave for each other.
+struct SplitArgs {
+  float *part_o, *part_ml;         // records [workgroup + head][R] of D floats / (reference, sum)
+  float *lse2;                     // [B Hkv][R]: log2 of the rows' sums, +inf for a row that sees nothing
+  float *logits;                   // nullable [B Hkv][R][capacity], times log2 e
+  Frag *frags;                     // nullable: operands and factors of the weights' second pass
+  float *factors;
+  const float *w_in;
+  float *w_out;
+  int workgroups;
+};
+
+// The weights of the positions n0 .. n0 + 3 from the rows' logits.
+__device__ __forceinline__ void weigh(const ns_kv_cache &c, const ns_kv_attn_desc &d, const SplitArgs &a, int64_t row, int n0, int length, int count,
+                                      const float *lse2 /* [R], in LDS */) {
+  const int G = d.heads / c.heads_kv, R = G * d.tokens;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (n0 < length) {
+    int t = 0, g = 0;
+    for (int r = 0; r < R; r++) {
+      const int limit = kv_seen(d, t, length, count);
+      const f32x4 z = *reinterpret_cast<const f32x4 *>(a.logits + (row * R + r) * c.capacity + n0);
+#pragma unroll
+      for (int i = 0; i < 4; i++) sum[i] += n0 + i < limit ? __builtin_amdgcn_exp2f(z[i] - lse2[r]) : 0.f;
+      if (++g == G) g = 0, t++;
+    }
+  }
+  const int64_t at = row * c.capacity + n0;
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    if (n0 + i < length || a.w_in != a.w_out) a.w_out[at + i] = (a.w_in ? a.w_in[at + i] : 0.f) + sum[i];
 }
 
-// tiles per workgroup
-__device__ __forceinline__ int64_t share_of(int64_t total, int workgroups) { return (total + workgroups - 1) / workgroups; }
+// Workgroups of four waves that a CU holds, by registers: more of them have more loads on their way.
+constexpr int per_cu(bool f32, int D, int NT) { return NT * D <= 128 || (!f32 && D == 128 && NT == 2) ? 2 : 1; }
 
-template <typename T> __device__ __forceinline__ f32x4 load4(const T *p);
-template <> __device__ __forceinline__ f32x4 load4<float>(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
-template <> __device__ __forceinline__ f32x4 load4<bf16_t>(const bf16_t *p) {
-  const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
-  return f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
-}
-
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
-}
-
-// PARTS: 1 for bf16 queries, 2 for fp32 ones (a number as the sum of two in fp16)
-template <typename T, int CODE, int D, int NT>
-__global__ __launch_bounds__(kThreads, NT * D <= 128 ? 2 : 1) void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
-                                                                    const int32_t *counts, float *part_o, float *part_ml, float *logits) {
+// T: float takes its queries, and the weights, as the sum of two fp16 numbers.  ALONE: a workgroup has a head to itself.
+template <typename T, int CODE, int D, int NT, int WAVES, bool ALONE>
+__global__ __launch_bounds__(WAVES * 64, ALONE ? (D == 256 ? 1 : 2) : per_cu(sizeof(T) == 4, D, NT))
+void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths, const int32_t *counts, T *out, float *lse, SplitArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1, KS = D / 32, DT = D / 16, VW = D / 64;   // k steps, channel tiles, dwords of V a token
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const int G = d.heads / c.heads_kv, R = G * d.tokens;
-  __shared__ __attribute__((aligned(16))) float sh_o[kWaves][16][D + 4];
-  __shared__ float sh_m[kWaves][16], sh_l[kWaves][16];
+  __shared__ __attribute__((aligned(16))) float sh_o[WAVES][16][D + 4];
+  __shared__ float sh_m[WAVES][16], sh_l[WAVES][16], sh_lse2[ALONE ? 16 * NT : 1];
 
-  const int64_t total = all_tiles(lengths, c.batch, c.capacity, lane) * c.heads_kv;
-  const int64_t share = share_of(total, gridDim.x);
-  int64_t u = share * blockIdx.x;
-  const int64_t u_end = min(u + share, total);
-  if (u >= u_end) return;
-  Place at = place_of(lengths, c.batch, c.capacity, c.heads_kv, u, lane);
+  const int lblock = 31 - __clz(c.block);
+  const Tiles tiles_all(lengths, c, lane);
+  int u = 0, u_end = 1;
+  if constexpr (!ALONE) {
+    const int share = tiles_all.share(gridDim.x), total = tiles_all.all();
+    if ((int)blockIdx.x > (total - 1) / share || total == 0) return;
+    u = share * (int)blockIdx.x;
+    u_end = min(u + share, total);
+  }
 
-  while (u < u_end) {
-    if (u >= at.first + (int64_t)at.tiles * c.heads_kv) at = place_of(lengths, c.batch, c.capacity, c.heads_kv, u, lane);
-    const int b = __builtin_amdgcn_readfirstlane(at.b), tiles = __builtin_amdgcn_readfirstlane(at.tiles);
-    const int h = __builtin_amdgcn_readfirstlane((int)((u - at.first) / tiles));
-    const int t0 = __builtin_amdgcn_readfirstlane((int)((u - at.first) - (int64_t)h * tiles));
-    const int t1 = (int)min((int64_t)tiles, t0 + (u_end - u));
-    const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
-    const int64_t row = (int64_t)b * c.heads_kv + h;
+  // ---- the piece of a head's tokens in hand, and codes on their way
+  int b = 0, h = 0, n_lo = 0, n_hi = 0, done = 1, length = 0, count = 0;
+  int64_t row = 0;
+  const uint8_t *kb = nullptr, *vb = nullptr;
+  const float *ks = nullptr, *vs = nullptr;
+  auto piece_at = [&](int tile) {
+    if constexpr (ALONE) {
+      b = (int)blockIdx.x / c.heads_kv;
+      h = (int)blockIdx.x - b * c.heads_kv;
+      length = kv_length(lengths, b, c.capacity);
+      n_hi = length;
+    } else {
+      int tiles, first;
+      tiles_all.place(tile, b, tiles, first);
+      h = (int)((unsigned)(tile - first) / (unsigned)tiles);
+      const int t0 = tile - first - h * tiles;
+      done = min(tiles - t0, u_end - tile);
+      length = kv_length(lengths, b, c.capacity);
+      n_lo = t0 * kTile;
+      n_hi = min(length, (t0 + done) * kTile);
+    }
+    count = kv_count(counts, b, d.tokens);
+    row = (int64_t)b * c.heads_kv + h;
+    kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
+    vb = static_cast<const uint8_t *>(c.v) + b * c.stride_b + h * c.stride_h;
+    ks = c.k_scale + row * (c.capacity >> lblock);
+    vs = c.v_scale + row * (c.capacity >> lblock);
+  };
+  const uint32_t k_off = (uint32_t)n16 * (uint32_t)c.stride_t + 16 * g, v_off = 4 * (uint32_t)g * (uint32_t)c.stride_t + (uint32_t)n16 * (D / 16);
+  u32x4 kw[2][D / 64];
+  uint32_t vw[8][VW];
+  float skey, sval;
+  auto fetch = [&](int n0) {
+    // (uniform bases and one offset: else the compiler advances an address of 64 bits for every load)
+    const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
+    const uint32_t ko = (uint32_t)opaque((int)k_off), vo = (uint32_t)opaque((int)v_off);
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int i = 0; i < D / 64; i++) kw[x][i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)x * 16 * c.stride_t + 64 * i + ko);
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const uint8_t *p = vp + (int64_t)((j >> 2) * 16 + (j & 3)) * c.stride_t + vo;
+      if constexpr (VW == 1) {
+        vw[j][0] = *reinterpret_cast<const uint32_t *>(p);
+      } else if constexpr (VW == 2) {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+        vw[j][0] = w[0]; vw[j][1] = w[1];
+      } else {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; i++) vw[j][i] = w[i];
+      }
+    }
+    skey = ks[n0 >> lblock];
+    sval = vs[n0 >> lblock];
+  };
+  constexpr int kStep = WAVES * kSub;
+  int n0 = 0;
+  auto begin = [&](int tile) {
+    piece_at(tile);
+    n0 = n_lo + wave * kSub;
+    if (n0 < n_hi) fetch(n0);
+  };
+  begin(u);
+  while (true) {
 
     // ---- the rows' queries
     Frag qf[NT][PARTS][KS];
     float factor[NT];
-    int limit[NT];
+    int limit[NT], least = 0x7fffffff;            // least: keys from here on are masked in some row
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
       const int r = nt * 16 + n16;
       const bool real = r < R;
       const int t = real ? r / G : 0;
       limit[nt] = real ? kv_seen(d, t, length, count) : 0;
+      if (real) least = min(least, limit[nt]);
       const T *p = q + b * d.q_stride_b + (int64_t)(h * G + (real ? r - t * G : 0)) * d.q_stride_h + (int64_t)t * d.q_stride_t;
       f32x4 x[D / 16];
       uint32_t most = 0;
@@ -146,19 +262,11 @@ __global__ __launch_bounds__(kThreads, NT * D <= 128 ? 2 : 1) void kv_attn_split
           }
         }
     }
-    int least = limit[0];                         // keys from here on are masked in some row
-#pragma unroll
-    for (int nt = 0; nt < NT; nt++)
-      if (nt * 16 + n16 < R) least = min(least, limit[nt]);
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
     least = __builtin_amdgcn_readfirstlane(least);
 
     // ---- its tokens, 32 at a time
-    const uint8_t *kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
-    const uint8_t *vb = static_cast<const uint8_t *>(c.v) + b * c.stride_b + h * c.stride_h;
-    const float *ks = c.k_scale + row * (c.capacity / c.block), *vs = c.v_scale + row * (c.capacity / c.block);
-    const int lblock = 31 - __clz(c.block);
     f32x4 o[NT][DT];
     float m[NT], l[NT];
 #pragma unroll
@@ -168,83 +276,64 @@ __global__ __launch_bounds__(kThreads, NT * D <= 128 ? 2 : 1) void kv_attn_split
 #pragma unroll
       for (int i = 0; i < DT; i++) o[nt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const uint32_t koff = (uint32_t)n16 * (uint32_t)c.stride_t + 16 * g, voff = 4 * (uint32_t)g * (uint32_t)c.stride_t + (uint32_t)n16 * (D / 16);
-    u32x4 kw[2][D / 64];
-    uint32_t vw[8][VW];
-    float skey, sval;
-    auto fetch = [&](int n0) {
-      const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
-#pragma unroll
-      for (int x = 0; x < 2; x++)
-#pragma unroll
-        for (int i = 0; i < D / 64; i++) kw[x][i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)x * 16 * c.stride_t + koff + 64 * i);
-#pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const uint8_t *p = vp + (int64_t)((j >> 2) * 16 + (j & 3)) * c.stride_t + voff;
-        if constexpr (VW == 1) {
-          vw[j][0] = *reinterpret_cast<const uint32_t *>(p);
-        } else if constexpr (VW == 2) {
-          const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
-          vw[j][0] = w[0]; vw[j][1] = w[1];
-        } else {
-          const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
-#pragma unroll
-          for (int i = 0; i < 4; i++) vw[j][i] = w[i];
-        }
-      }
-      skey = ks[n0 >> lblock];
-      sval = vs[n0 >> lblock];
-    };
-    const int end = min(length, t1 * kTile);
-    int n0 = t0 * kTile + wave * kSub;
-    if (n0 < end) fetch(n0);
-    for (; n0 < end; n0 += kTile) {
-      // K to fp16; V's dwords on to other registers, so that the next tokens' loads can be under way
-      Frag kf[2][KS];
-#pragma unroll
-      for (int x = 0; x < 2; x++)
-#pragma unroll
-        for (int s = 0; s < KS; s++) kf[x][s] = kv_frag<CODE>(kw[x][s / 2][2 * (s % 2)], kw[x][s / 2][2 * (s % 2) + 1]);
+    for (; n0 < n_hi; n0 += kStep) {
       const bool edge = n0 + kSub > least;
-      uint32_t vt[VW][8];
+      uint32_t vt[VW][8];                           // V's dwords on to other registers, so that the next tokens' loads can be under way
 #pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const bool there = !edge || n0 + (j >> 2) * 16 + 4 * g + (j & 3) < length;    // what lies behind may be NaN
+      for (int j = 0; j < 8; j++)
 #pragma unroll
-        for (int i = 0; i < VW; i++) vt[i][j] = there ? vw[j][i] : 0u;
+        for (int i = 0; i < VW; i++) vt[i][j] = vw[j][i];
+      if (edge) {                                   // what lies behind the length may be NaN
+        asm volatile("; edge");                     // (a branch, not selects in every step)
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+#pragma unroll
+          for (int i = 0; i < VW; i++) vt[i][j] = n0 + (j >> 2) * 16 + 4 * g + (j & 3) < length ? vt[i][j] : 0u;
       }
       const float sk = skey, sv = sval;
-      if (n0 + kTile < end) fetch(n0 + kTile);
+      f32x4 sx[NT][2];
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        Frag kf[KS];
+#pragma unroll
+        for (int k = 0; k < KS; k++) kf[k] = kv_frag<CODE>(kw[x][k / 2][2 * (k % 2)], kw[x][k / 2][2 * (k % 2) + 1]);
+        if (x == 1 && n0 + kStep < n_hi) fetch(n0 + kStep);      // (two steps ahead instead of one: no faster)
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+          sx[nt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int pt = PARTS - 1; pt >= 0; pt--)
+#pragma unroll
+            for (int k = 0; k < KS; k++) sx[nt][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[k].v, qf[nt][pt][k].v, sx[nt][x], 0, 0, 0);
+        }
+        if (NT > 1) __builtin_amdgcn_sched_barrier(0);
+      }
 
       Frag pf[NT][PARTS];
       float svr[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; nt++) {
-        f32x4 s[2];
-#pragma unroll
-        for (int x = 0; x < 2; x++) {
-          s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int pt = PARTS - 1; pt >= 0; pt--)
-#pragma unroll
-            for (int k = 0; k < KS; k++) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x][k].v, qf[nt][pt][k].v, s[x], 0, 0, 0);
-        }
+        const f32x4 (&s)[2] = sx[nt];
         const float f = factor[nt] * sk;
-        if (logits && nt * 16 + n16 < R) {
+        if (a.logits && nt * 16 + n16 < R) {
 #pragma unroll
           for (int x = 0; x < 2; x++)
-            *reinterpret_cast<f32x4 *>(logits + (row * R + nt * 16 + n16) * c.capacity + n0 + 16 * x + 4 * g) = s[x] * f;
+            *reinterpret_cast<f32x4 *>(a.logits + (row * R + nt * 16 + n16) * c.capacity + n0 + 16 * x + 4 * g) = s[x] * f;
         }
         const bool fresh = m[nt] == -INFINITY;                                         // this row has seen no key yet
         const float ref = fresh ? 0.f : m[nt];
         float z[8], top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-          z[i] = __builtin_fmaf(s[i / 4][i % 4], f, -ref);
-          if (edge) z[i] = n0 + (i / 4) * 16 + 4 * g + i % 4 < limit[nt] ? z[i] : -INFINITY;
-          top = fmaxf(top, z[i]);
+        for (int i = 0; i < 8; i++) z[i] = __builtin_fmaf(s[i / 4][i % 4], f, -ref);
+        svr[nt] = sv;
+        if (edge) {
+          asm volatile("; edge");
+#pragma unroll
+          for (int i = 0; i < 8; i++) z[i] = n0 + (i / 4) * 16 + 4 * g + i % 4 < limit[nt] ? z[i] : -INFINITY;
+          svr[nt] = n0 >= limit[nt] ? 0.f : sv;                                        // a NaN block is NaN for those who see it
         }
-        svr[nt] = edge && n0 >= limit[nt] ? 0.f : sv;                                  // a NaN block is NaN for those who see it
+#pragma unroll
+        for (int i = 0; i < 8; i++) top = fmaxf(top, z[i]);
         if (__any(top > kRoom || (fresh && top > -INFINITY))) {
           top = half_swap_max(row_swap_max(top));
           const bool moved = top > kRoom || (fresh && top > -INFINITY);
@@ -281,17 +370,21 @@ __global__ __launch_bounds__(kThreads, NT * D <= 128 ? 2 : 1) void kv_attn_split
         for (int j = 0; j < 4; j++)
 #pragma unroll
           for (int nt = 0; nt < NT; nt++) {
-            f32x4 a = {0.f, 0.f, 0.f, 0.f};
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int pt = PARTS - 1; pt >= 0; pt--) a = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j].v, pf[nt][pt].v, a, 0, 0, 0);
+            for (int pt = PARTS - 1; pt >= 0; pt--) y = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[j].v, pf[nt][pt].v, y, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; e++) o[nt][4 * i + j][e] = __builtin_fmaf(a[e], svr[nt], o[nt][4 * i + j][e]);
+            for (int e = 0; e < 4; e++) o[nt][4 * i + j][e] = __builtin_fmaf(y[e], svr[nt], o[nt][4 * i + j][e]);
           }
+        if (VW > 1) __builtin_amdgcn_sched_barrier(0);
       }
     }
 
-    // ---- the four waves' results together, and out: record (blockIdx.x + row) of the joined head
-    const int64_t slot = (int64_t)blockIdx.x + row;
+    // ---- the next piece's first tokens on their way; the waves' results together, and out: record (blockIdx.x + row) of the joined head
+    const int64_t out_row = row, slot = (int64_t)blockIdx.x + row;
+    const int out_b = b, out_h = h, out_length = length, out_count = count;
+    u += done;
+    if (!ALONE && u < u_end) begin(u);
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
       const float ls = half_swap_sum(row_swap_sum(l[nt]));
@@ -306,171 +399,222 @@ __global__ __launch_bounds__(kThreads, NT * D <= 128 ? 2 : 1) void kv_attn_split
         for (int i = 0; i < DT; i += 4)
           *reinterpret_cast<f32x4 *>(&sh_o[wave][n16][(4 * g + e) * DT + i]) = f32x4{o[nt][i][e], o[nt][i + 1][e], o[nt][i + 2][e], o[nt][i + 3][e]};
       __syncthreads();
-      const int tid = threadIdx.x;
-      for (int x = tid; x < 16 * D / 4; x += kThreads) {
+      for (int x = tid; x < 16 * D / 4; x += WAVES * 64) {
         const int n = x / (D / 4), dd = x % (D / 4) * 4, r = nt * 16 + n;
         if (r < R) {
           float M = sh_m[0][n];
 #pragma unroll
-          for (int w = 1; w < kWaves; w++) M = fmaxf(M, sh_m[w][n]);
-          f32x4 a = {0.f, 0.f, 0.f, 0.f};
+          for (int w = 1; w < WAVES; w++) M = fmaxf(M, sh_m[w][n]);
+          f32x4 y = {0.f, 0.f, 0.f, 0.f};
           float ll = 0.f;
 #pragma unroll
-          for (int w = 0; w < kWaves; w++) {
-            const float fade = sh_m[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sh_m[w][n] - M);
-            if (sh_m[w][n] != -INFINITY) a += *reinterpret_cast<const f32x4 *>(&sh_o[w][n][dd]) * fade;
-            ll += sh_l[w][n] * fade;
+          for (int w = 0; w < WAVES; w++) {
+            const float fade = __builtin_amdgcn_exp2f(sh_m[w][n] - M);
+            if (sh_m[w][n] != -INFINITY) {
+              y += *reinterpret_cast<const f32x4 *>(&sh_o[w][n][dd]) * fade;
+              ll += sh_l[w][n] * fade;
+            }
           }
-          *reinterpret_cast<f32x4 *>(part_o + (slot * R + r) * D + dd) = a;
-          if (dd == 0) *reinterpret_cast<f32x2 *>(part_ml + (slot * R + r) * 2) = f32x2{M, ll};
+          if constexpr (ALONE) {
+            const bool some = M != -INFINITY;
+            const int t = r / G, hq = out_h * G + r - t * G;
+            const float inv = some ? 1.f / ll : 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; e++) y[e] = some ? y[e] * inv : 0.f;
+            store4(out + out_b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd, y);
+            if (dd == 0) {
+              const float z2 = some ? M + __log2f(ll) : -INFINITY;
+              if (lse) lse[((int64_t)out_b * d.heads + hq) * d.tokens + t] = z2 * kLn2;
+              sh_lse2[r] = some ? z2 : INFINITY;
+              if (a.frags) a.lse2[out_row * R + r] = sh_lse2[r];
+            }
+          } else {
+            *reinterpret_cast<f32x4 *>(a.part_o + (slot * R + r) * D + dd) = y;
+            if (dd == 0) *reinterpret_cast<f32x2 *>(a.part_ml + (slot * R + r) * 2) = f32x2{M, ll};
+          }
         }
       }
       __syncthreads();
     }
-    u += t1 - t0;
+    if constexpr (ALONE) {
+      if (a.logits)
+        for (int n = tid * 4; n < c.capacity && (n < out_length || a.w_in != a.w_out); n += WAVES * 64 * 4)
+          weigh(c, d, a, out_row, n, out_length, out_count, sh_lse2);
+    }
+    if (ALONE || u >= u_end) break;
   }
 }
 
-// One workgroup per row: the joined result of its head's partial ones.
+// The first R workgroups of a head: a row's joined result each.  The others: the weights of 1024 positions each from the rows'
+// logits, or the operands for the weights' second pass.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, int workgroups,
-                                                                const float *part_o, const float *part_ml, T *out, float *lse, float *lse2) {
-  const int tid = threadIdx.x, lane = tid & 63, D = c.head_dim;
+__global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
+                                                                const int32_t *counts, T *out, float *lse, SplitArgs a) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, D = c.head_dim;
   const int G = d.heads / c.heads_kv, R = G * d.tokens;
-  const int r = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int x = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int64_t row = (int64_t)b * c.heads_kv + h;
-  __shared__ float sh[kThreads * 4], sh_ml[kThreads * 2];
+  __shared__ __attribute__((aligned(16))) float sh[kThreads * 4];
+  __shared__ float fades[kMostParts], sh_w[2 * kWaves], lse2[64];
+  if (x >= R && a.frags) {
+    const int tile = (x - R) * kWaves + wave;
+    if (tile < (R + 15) / 16) kv_rows_tile(c, d, q, b, h, tile, lane, a.frags, a.factors);
+    return;
+  }
 
-  const int64_t total = all_tiles(lengths, c.batch, c.capacity, lane) * c.heads_kv;
-  const int64_t share = max((int64_t)1, share_of(total, workgroups));
-  int64_t before = 0;
-  for (int x = 0; x < b; x += 64) before += wave_total(x + lane < b ? tiles_of(lengths, x + lane, c.batch, c.capacity) : 0);
-  const int tiles = tiles_of(lengths, b, c.batch, c.capacity);
-  const int64_t lo = before * c.heads_kv + (int64_t)h * tiles;
-  const int first = (int)(lo / share), parts = tiles ? (int)((lo + tiles - 1) / share) - first + 1 : 0;
+  // this head's records
+  const Tiles tiles_all(lengths, c, lane);
+  const int share = tiles_all.share(a.workgroups);
+  const int tiles = tiles_of(lengths, b, c.batch, c.capacity), lo = tiles_all.before(b) + h * tiles;
+  const int first = lo / share, parts = tiles ? (lo + tiles - 1) / share - first + 1 : 0;
   const int64_t slot = first + row;
 
-  // the largest reference and the sum, by the wave's lanes, the same in every wave
-  float M = -INFINITY;
-  for (int p = lane; p < parts; p += 64) M = fmaxf(M, part_ml[((slot + p) * R + r) * 2]);
-  M = wave_max(M);
-  const int quads = D / 4, slices = kThreads / quads, s = tid / quads, dd = tid % quads * 4;
-  f32x4 a = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.f;
-  for (int p = s; p < parts; p += slices) {
-    const float *ml = part_ml + ((slot + p) * R + r) * 2;
-    if (ml[0] != -INFINITY) {
-      const float fade = __builtin_amdgcn_exp2f(ml[0] - M);
-      a += *reinterpret_cast<const f32x4 *>(part_o + ((slot + p) * R + r) * D + dd) * fade;
-      L += ml[1] * fade;
+  if (x >= R) {
+    for (int r = wave; r < R; r += kWaves) {
+      float M = -INFINITY, L = 0.f;
+      for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.part_ml[((slot + p) * R + r) * 2]);
+      M = wave_max(M);
+      for (int p = lane; p < parts; p += 64) {
+        const f32x2 ml = *reinterpret_cast<const f32x2 *>(a.part_ml + ((slot + p) * R + r) * 2);
+        L += ml[0] == -INFINITY ? 0.f : ml[1] * __builtin_amdgcn_exp2f(ml[0] - M);
+      }
+      L = wave_sum(L);
+      if (lane == 0) lse2[r] = M == -INFINITY ? INFINITY : M + __log2f(L);
     }
+    __syncthreads();
+    const int n = ((x - R) * kThreads + tid) * 4, length = kv_length(lengths, b, c.capacity);
+    if (n < c.capacity && (n < length || a.w_in != a.w_out)) weigh(c, d, a, row, n, length, kv_count(counts, b, d.tokens), lse2);
+    return;
   }
-  *reinterpret_cast<f32x4 *>(&sh[tid * 4]) = a;
-  sh_ml[tid] = L;
+
+  const int r = x, quads = D / 4, slices = kThreads / quads, s = tid / quads, dd = tid % quads * 4;
+  const float *records = a.part_o + (slot * R + r) * D + dd, *mls = a.part_ml + (slot * R + r) * 2;
+  constexpr int kAhead = 4;                         // records that are loaded before it is known what they are multiplied with
+  f32x4 v[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; i++) v[i] = s + i * slices < parts ? *reinterpret_cast<const f32x4 *>(records + (int64_t)(s + i * slices) * R * D) : f32x4{0.f, 0.f, 0.f, 0.f};
+  float M = -INFINITY, L = 0.f;
+  f32x2 own = {-INFINITY, 0.f};                     // (as a rule there are no more records than threads)
+  for (int p = tid; p < parts; p += kThreads) {
+    own = *reinterpret_cast<const f32x2 *>(mls + (int64_t)p * R * 2);
+    M = fmaxf(M, own[0]);
+  }
+  M = wave_max(M);
+  if (lane == 0) sh_w[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sh_w[0], sh_w[1]), fmaxf(sh_w[2], sh_w[3]));
+  for (int p = tid; p < parts; p += kThreads) {
+    if (parts > kThreads) own = *reinterpret_cast<const f32x2 *>(mls + (int64_t)p * R * 2);
+    const float fade = own[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(own[0] - M);
+    fades[p] = fade;
+    L += own[0] == -INFINITY ? 0.f : own[1] * fade;
+  }
+  L = wave_sum(L);
+  if (lane == 0) sh_w[kWaves + wave] = L;
+  __syncthreads();
+  L = (sh_w[kWaves] + sh_w[kWaves + 1]) + (sh_w[kWaves + 2] + sh_w[kWaves + 3]);
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kAhead; i++)
+    if (s + i * slices < parts) y += v[i] * fades[s + i * slices];
+#pragma unroll 4
+  for (int p = s + kAhead * slices; p < parts; p += slices) y += *reinterpret_cast<const f32x4 *>(records + (int64_t)p * R * D) * fades[p];
+  *reinterpret_cast<f32x4 *>(&sh[tid * 4]) = y;
   __syncthreads();
   if (tid < quads) {
-    L = sh_ml[tid];
-    for (int x = 1; x < slices; x++) {
-      a += *reinterpret_cast<const f32x4 *>(&sh[(x * quads + tid) * 4]);
-      L += sh_ml[x * quads + tid];
-    }
+    for (int i = 1; i < slices; i++) y += *reinterpret_cast<const f32x4 *>(&sh[(i * quads + tid) * 4]);
     const bool some = M != -INFINITY;
     const float inv = some ? 1.f / L : 0.f;
     const int t = r / G, hq = h * G + r - t * G;
-    T *to = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd;
 #pragma unroll
-    for (int e = 0; e < 4; e++) a[e] = some ? a[e] * inv : 0.f;
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<f32x4 *>(to) = a;
-    } else {
-      *reinterpret_cast<u32x2 *>(to) = u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
-    }
+    for (int e = 0; e < 4; e++) y[e] = some ? y[e] * inv : 0.f;
+    store4(out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd, y);
     if (tid == 0) {
       const float z2 = some ? M + __log2f(L) : -INFINITY;
       if (lse) lse[((int64_t)b * d.heads + hq) * d.tokens + t] = z2 * kLn2;
-      if (lse2) lse2[row * R + r] = z2;
+      if (a.frags) a.lse2[row * R + r] = some ? z2 : INFINITY;
     }
   }
 }
 
-// The weights that every position was given, from the rows' logits; four positions a thread.
-__global__ __launch_bounds__(kThreads) void kv_weights_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
-                                                              const float *logits, const float *lse2, const float *w_in, float *w_out) {
-  const int h = blockIdx.y, b = blockIdx.z, n0 = (int)(blockIdx.x * kThreads + threadIdx.x) * 4;
-  const int G = d.heads / c.heads_kv, R = G * d.tokens;
-  const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
-  if (n0 >= c.capacity || (n0 >= length && w_in == w_out)) return;
-  const int64_t row = (int64_t)b * c.heads_kv + h;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  if (n0 < length)
-    for (int r = 0; r < R; r++) {
-      const int limit = kv_seen(d, r / G, length, count);
-      const f32x4 z = *reinterpret_cast<const f32x4 *>(logits + (row * R + r) * c.capacity + n0);
-      const float ref = lse2[row * R + r];
-#pragma unroll
-      for (int i = 0; i < 4; i++) sum[i] += n0 + i < limit ? __builtin_amdgcn_exp2f(z[i] - ref) : 0.f;
-    }
-  const int64_t at = row * c.capacity + n0;
-  for (int i = 0; i < 4; i++)
-    if (n0 + i < length || w_in != w_out) w_out[at + i] = (w_in ? w_in[at + i] : 0.f) + sum[i];
-}
-
-// ---- host side of the split kernel
+// ---- host side
 
 int rows_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return d.heads / c.heads_kv * d.tokens; }
 
-// Row tiles of 16 that the split kernel has registers for
-int most_tiles(int head_dim, int dtype) {
-  if (dtype == NS_F32) return head_dim == 64 ? 4 : head_dim == 128 ? 2 : 1;
-  return head_dim == 256 ? 1 : 4;
-}
+// Row tiles of 16 that there are registers for
+constexpr int most_tiles(int head_dim, int dtype) { (void)dtype; return head_dim == 256 ? 1 : head_dim == 128 ? 2 : 4; }
 bool few_rows(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return rows_of(c, d) <= 16 * most_tiles(c.head_dim, d.dtype); }
 
-struct SplitLayout { size_t o, ml, lse2, logits, total; int workgroups; };
-SplitLayout split_layout(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
-  SplitLayout w;
-  w.workgroups = ((rows_of(c, d) + 15) / 16 * c.head_dim <= 128 ? 2 : 1) * device_cu_count();
-  const size_t rows = rows_of(c, d), heads = (size_t)c.batch * c.heads_kv, slots = (size_t)w.workgroups + heads;
+// Logits are 8 bytes a row and key, written and read; K read again D bytes a key.
+bool by_logits(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return 8 * rows_of(c, d) <= c.head_dim; }
+bool alone(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
+  return rows_of(c, d) <= 16 && c.capacity <= ((int64_t)c.batch * c.heads_kv >= device_cu_count() ? 4096 : 1024);
+}
+
+struct Layout { size_t o, ml, lse2, logits, frags, factors, total; int workgroups; };
+Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
+  Layout w{};
+  const bool shared = !alone(c, d), logits = weights && by_logits(c, d), again = weights && !logits;
+  const size_t rows = rows_of(c, d), heads = (size_t)c.batch * c.heads_kv;
+  const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  w.workgroups = std::min(per_cu(d.dtype == NS_F32, c.head_dim, nt) * device_cu_count(), kMostParts);
+  const size_t slots = (size_t)w.workgroups + heads;
   size_t off = 0;
-  w.o = off;
-  off += align_up(slots * rows * c.head_dim * 4, 256);
-  w.ml = off;
-  off += align_up(slots * rows * 8, 256);
-  w.lse2 = off;
-  off += align_up(heads * rows * 4, 256);
-  w.logits = off;
-  if (weights) off += align_up(heads * rows * (size_t)c.capacity * 4, 256);
+  auto take = [&](bool wanted, size_t bytes) {
+    const size_t was = off;
+    off += wanted ? align_up(bytes, 256) : 0;
+    return was;
+  };
+  w.o = take(shared, slots * rows * c.head_dim * 4);
+  w.ml = take(shared, slots * rows * 8);
+  w.lse2 = take(again, heads * rows * 4);
+  w.logits = take(logits, heads * rows * (size_t)c.capacity * 4);
+  w.frags = take(again, again ? kv_rows_frag_bytes(c, d) : 0);
+  w.factors = take(again, again ? kv_rows_factor_bytes(c, d) : 0);
   w.total = off;
   return w;
 }
 
 template <typename T, int CODE, int D, int NT>
 ns_status launch_split(const KvAttnArgs &a) {
-  const SplitLayout w = split_layout(a.c, a.d, a.w_out != nullptr);
-  float *po = reinterpret_cast<float *>(a.ws + w.o), *pml = reinterpret_cast<float *>(a.ws + w.ml);
-  float *lse2 = reinterpret_cast<float *>(a.ws + w.lse2), *logits = a.w_out ? reinterpret_cast<float *>(a.ws + w.logits) : nullptr;
-  hipLaunchKernelGGL((kv_attn_split_kernel<T, CODE, D, NT>), dim3((unsigned)w.workgroups), dim3(kThreads), 0, a.stream, a.c, a.d,
-                     static_cast<const T *>(a.q), a.lengths, a.counts, po, pml, logits);
+  const ns_kv_cache &c = a.c;
+  const bool weights = a.w_out != nullptr, logits = weights && by_logits(c, a.d), again = weights && !logits;
+  const Layout w = layout_of(c, a.d, weights);
+  auto at = [&](size_t off) { return reinterpret_cast<float *>(a.ws + off); };
+  SplitArgs s{at(w.o), at(w.ml), at(w.lse2), logits ? at(w.logits) : nullptr, again ? reinterpret_cast<Frag *>(a.ws + w.frags) : nullptr, at(w.factors),
+              a.w_in, a.w_out, w.workgroups};
+  const T *q = static_cast<const T *>(a.q);
+  T *out = static_cast<T *>(a.out);
+  if constexpr (NT == 1)
+    if (alone(c, a.d)) {
+      constexpr int WAVES = D == 256 ? 4 : 8;       // (LDS)
+      hipLaunchKernelGGL((kv_attn_split_kernel<T, CODE, D, NT, WAVES, true>), dim3((unsigned)(c.batch * c.heads_kv)), dim3(WAVES * 64), 0, a.stream, c, a.d, q,
+                         a.lengths, a.counts, out, a.lse, s);
+      const ns_status st = check_launch("kv_attn_split_kernel");
+      if (st != NS_OK || !again) return st;
+      return launch_kv_weights_again(a, s.frags, s.factors, s.lse2, true);
+    }
+  hipLaunchKernelGGL((kv_attn_split_kernel<T, CODE, D, NT, kWaves, false>), dim3((unsigned)w.workgroups), dim3(kThreads), 0, a.stream, c, a.d, q, a.lengths,
+                     a.counts, out, a.lse, s);
   ns_status st = check_launch("kv_attn_split_kernel");
   if (st != NS_OK) return st;
-  hipLaunchKernelGGL((kv_attn_join_kernel<T>), dim3((unsigned)rows_of(a.c, a.d), (unsigned)a.c.heads_kv, (unsigned)a.c.batch), dim3(kThreads), 0, a.stream,
-                     a.c, a.d, a.lengths, w.workgroups, po, pml, static_cast<T *>(a.out), a.lse, lse2);
+  const int rows = rows_of(c, a.d), more = logits ? (c.capacity + 4 * kThreads - 1) / (4 * kThreads) : again ? 1 : 0;
+  hipLaunchKernelGGL((kv_attn_join_kernel<T>), dim3((unsigned)(rows + more), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(kThreads), 0, a.stream,
+                     c, a.d, q, a.lengths, a.counts, out, a.lse, s);
   st = check_launch("kv_attn_join_kernel");
-  if (st != NS_OK || !a.w_out) return st;
-  hipLaunchKernelGGL(kv_weights_kernel, dim3((unsigned)((a.c.capacity + 4 * kThreads - 1) / (4 * kThreads)), (unsigned)a.c.heads_kv, (unsigned)a.c.batch),
-                     dim3(kThreads), 0, a.stream, a.c, a.d, a.lengths, a.counts, logits, lse2, a.w_in, a.w_out);
-  return check_launch("kv_weights_kernel");
+  if (st != NS_OK || !again) return st;
+  return launch_kv_weights_again(a, s.frags, s.factors, s.lse2, false);
 }
 
 template <typename T, int CODE, int D>
 ns_status launch_tiles(const KvAttnArgs &a) {
-  constexpr int most = sizeof(T) == 4 ? (D == 64 ? 4 : D == 128 ? 2 : 1) : D == 256 ? 1 : 4;
+  constexpr int most = most_tiles(D, sizeof(T) == 4 ? NS_F32 : NS_BF16);
   const int nt = (rows_of(a.c, a.d) + 15) / 16;
-  if (nt <= 1) return launch_split<T, CODE, D, 1>(a);
   if constexpr (most >= 4)
     if (nt > 2) return launch_split<T, CODE, D, 4>(a);
-  if constexpr (most >= 2) return launch_split<T, CODE, D, 2>(a);
-  return NS_ERR_UNSUPPORTED;
+  if constexpr (most >= 2)
+    if (nt > 1) return launch_split<T, CODE, D, 2>(a);
+  return launch_split<T, CODE, D, 1>(a);
 }
 
 template <typename T, int CODE>
@@ -482,8 +626,7 @@ ns_status launch_any(const KvAttnArgs &a) {
 }  // namespace
 
 size_t kv_attn_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
-  if (!few_rows(c, d)) return kv_prompt_workspace_bytes(c, d, weights);
-  return split_layout(c, d, weights).total;
+  return few_rows(c, d) ? layout_of(c, d, weights).total : kv_prompt_workspace_bytes(c, d, weights);
 }
 
 ns_status launch_kv_attn(const KvAttnArgs &a) {

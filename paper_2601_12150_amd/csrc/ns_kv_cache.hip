@@ -20,9 +20,6 @@ template <> struct Row8<bf16_t> {
   __device__ __forceinline__ void zero() { w = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ f32x4 half(int i) const { return f32x4{bf16_lo(w[2 * i]), bf16_hi(w[2 * i]), bf16_lo(w[2 * i + 1]), bf16_hi(w[2 * i + 1])}; }
 };
-__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
-__device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
-
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // One workgroup per block of tokens that a sequence's new tokens may touch, head, and keys or values.  The scale needs the

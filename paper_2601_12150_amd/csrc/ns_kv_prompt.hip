@@ -17,22 +17,6 @@ namespace ns {
 namespace {
 
 constexpr int kKeys = 64;
-// Weights are 2^(z - m + 11) in fp16, m a logit near the largest so far, which is moved up before they pass 2^15: a weight that is the
-// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.
-constexpr float kLift = 11.f, kRoom = 15.f;
-
-typedef __attribute__((address_space(3))) uint8_t lds_t;
-
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
-}
-template <typename T> __device__ __forceinline__ f32x4 load4(const T *p);
-template <> __device__ __forceinline__ f32x4 load4<float>(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
-template <> __device__ __forceinline__ f32x4 load4<bf16_t>(const bf16_t *p) {
-  const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
-  return f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
-}
-
 // 16-byte pieces of a row of K (D / 8 of them) and of V^T (8) in LDS.  V^T's rows are written four channels apart and read one
 // apart: the exchange of its pieces is one to one in bits 0..2 of the channel as well as in bits 2..4.  Exchanges are exclusive ors, so
 // that of another piece of the row the address is another exclusive or.
@@ -404,10 +388,7 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
 #pragma unroll
       for (int j = 0; j < 4; j++) y[j] = some ? o[i][e + j] * by : 0.f;
       T *p = to + 32 * i + 2 * e + 4 * hh;
-      if constexpr (sizeof(T) == 4)
-        *reinterpret_cast<f32x4 *>(p) = y;
-      else
-        *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+      store4(p, y);
     }
   if (hh == 0 && part == 0) {
     const float z2 = some ? m + __log2f(l) : -INFINITY;
@@ -443,10 +424,7 @@ __global__ __launch_bounds__(256) void kv_prompt_join_kernel(ns_kv_cache c, ns_k
 #pragma unroll
     for (int j = 0; j < 4; j++) y[j] = some ? y[j] * inv : 0.f;
     T *p = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd;
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<f32x4 *>(p) = y;
-    else
-      *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    store4(p, y);
   }
   if (lane == 0) {
     const float z2 = some ? M + __log2f(L) : -INFINITY;
@@ -456,136 +434,110 @@ __global__ __launch_bounds__(256) void kv_prompt_join_kernel(ns_kv_cache c, ns_k
 }
 
 // ---- the weights that every position was given: exp(logit - lse) summed over the rows, with K read again.  The rows' operands and
-// factors are made once (kv_weights_rows_kernel); a wave then has 64 keys in registers and takes 32 rows at a time from the L2.
+// factors are made once (kv_rows_tile); a wave then has 16 KX keys in registers and takes 16 rows at a time from the L2.
 
-// Channels of the step s = 2 i + f that lane (n, hh) has: 32 i + 16 hh + 8 f + j, so that 16 bytes of codes are two operands.
 template <typename T>
 __global__ __launch_bounds__(256) void kv_weights_rows_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, Frag *frags, float *factors) {
-  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
-  const int lane = threadIdx.x & 63, n32 = lane & 31, hh = lane >> 5, KS = c.head_dim / 16;
-  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 31) / 32;
-  const int tile = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
-  if (tile >= tiles) return;
-  const int64_t row = (int64_t)b * c.heads_kv + h;
-  const int r = tile * 32 + n32;
-  const bool real = r < R;
-  const int t = real ? r / G : 0;
-  const T *p = q + b * d.q_stride_b + (int64_t)(h * G + (real ? r - t * G : 0)) * d.q_stride_h + (int64_t)t * d.q_stride_t + 16 * hh;
-  uint32_t most = 0;
-  for (int i = 0; i < KS / 2; i++)
-    for (int k = 0; k < 4; k++) {
-      const f32x4 x = load4(p + 32 * i + 4 * k);
-#pragma unroll
-      for (int j = 0; j < 4; j++) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
-    }
-  most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-  const int shift = kv_row_shift(most);
-  if (hh == 0) factors[row * tiles * 32 + r] = real ? ldexpf(d.scale * kLog2e, -shift) : 0.f;
-  for (int s = 0; s < KS; s++) {
-    Frag f[PARTS];
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      const f32x4 x = load4(p + 32 * (s / 2) + 8 * (s % 2) + 4 * k);
-#pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        const float x0 = real ? ldexpf(x[j], shift) : 0.f, x1 = real ? ldexpf(x[j + 1], shift) : 0.f;
-        f[0].w[2 * k + j / 2] = pack_f16(x0, x1);
-        if (PARTS == 2) {
-          const f16x2 w = __builtin_bit_cast(f16x2, f[0].w[2 * k + j / 2]);
-          f[PARTS - 1].w[2 * k + j / 2] = pack_f16(x0 - (float)w[0], x1 - (float)w[1]);
-        }
-      }
-    }
-#pragma unroll
-    for (int pt = 0; pt < PARTS; pt++) frags[(((row * tiles + tile) * PARTS + pt) * KS + s) * 64 + lane] = f[pt];
-  }
+  const int tile = blockIdx.x * 4 + (threadIdx.x >> 6), R = d.heads / c.heads_kv * d.tokens;
+  if (tile < (R + 15) / 16) kv_rows_tile(c, d, q, blockIdx.z, blockIdx.y, tile, threadIdx.x & 63, frags, factors);
 }
 
-template <int PARTS, int CODE, int D>
+// KX: tiles of 16 keys that a wave has: four for many rows (an operand of theirs serves all), two for few (more waves, more loads on
+// their way)
+template <int PARTS, int CODE, int D, int KX>
 __global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
                                                              const Frag *frags, const float *factors, const float *lse2, const float *w_in,
                                                              float *w_out) {
-  constexpr int KS = D / 16;
-  const int lane = threadIdx.x & 63, n32 = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 31) / 32;
-  const int h = blockIdx.y, b = blockIdx.z, n0 = (int)blockIdx.x * 256 + wave * 64;
+  constexpr int KS = D / 32, kKeysOf = 16 * KX;
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 15) / 16, lblock = 31 - __clz(c.block);
+  const int h = blockIdx.y, b = blockIdx.z, n0 = ((int)blockIdx.x * 4 + wave) * kKeysOf;
+  __shared__ float sums[4][kKeysOf][17];
   const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
   const int64_t row = (int64_t)b * c.heads_kv + h;
   if (n0 >= c.capacity) return;
   float sum = 0.f;                                  // of the key n0 + lane
-  if (n0 < length) {
-    Frag kf[2][KS];
-    float sk[2];
+  // causal: the first row that sees key n0 is that of the query at its position
+  const int first = d.causal ? (int)min((int64_t)max(0, n0 - (length - count)) * G / 16, (int64_t)tiles) : 0;
+  const int last = min(tiles, (count * G + 15) / 16);
+  if (n0 < length && first < last) {
+    const uint8_t *kp = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h + (int64_t)n0 * c.stride_t;
+    const uint32_t off = (uint32_t)n16 * (uint32_t)c.stride_t + 16 * g;
+    u32x4 kw[KX][D / 64];
+    float sk[KX];
 #pragma unroll
-    for (int x = 0; x < 2; x++) {
-      const int key = min(n0 + 32 * x + n32, c.capacity - 1);
-      const uint8_t *p = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h + (int64_t)key * c.stride_t + 16 * hh;
+    for (int x = 0; x < KX; x++) {
+      // (tiles behind the capacity take the last one again; they are masked)
+      const int at = min(16 * x, c.capacity - 16 - n0);
 #pragma unroll
-      for (int i = 0; i < KS / 2; i++) {
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(p + 32 * i);
-        kf[x][2 * i] = kv_frag<CODE>(w[0], w[1]);
-        kf[x][2 * i + 1] = kv_frag<CODE>(w[2], w[3]);
-      }
-      sk[x] = c.k_scale[row * (c.capacity / c.block) + min(n0 + 32 * x, c.capacity - 32) / c.block];
+      for (int i = 0; i < D / 64; i++) kw[x][i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)at * c.stride_t + 64 * i + off);
+      sk[x] = c.k_scale[row * (c.capacity >> lblock) + ((n0 + at) >> lblock)];
     }
-    f32x16 acc[2];
+    const Frag *qp = frags + (row * tiles * PARTS) * KS * 64 + lane;
+    Frag next[PARTS * KS];
+    float fr, ref;
+    auto load_rows = [&](int tile) {
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+      for (int k = 0; k < PARTS * KS; k++) next[k] = qp[((int64_t)tile * PARTS * KS + k) * 64];
+      const int r = tile * 16 + n16;
+      fr = factors[row * tiles * 16 + r];
+      ref = r < R ? lse2[row * R + r] : INFINITY;
+    };
+    load_rows(first);
+    Frag kf[KX][KS];
 #pragma unroll
-      for (int e = 0; e < 16; e++) acc[x][e] = 0.f;
-    // causal: the first row that sees key n0 is that of the query at its position
-    const int first = d.causal ? max(0, n0 - (length - count)) * G / 32 : 0;
-    const int last = min(tiles, (count * G + 31) / 32);
+    for (int x = 0; x < KX; x++)
+#pragma unroll
+      for (int k = 0; k < KS; k++) kf[x][k] = kv_frag<CODE>(kw[x][k / 2][2 * (k % 2)], kw[x][k / 2][2 * (k % 2) + 1]);
+    f32x4 acc[KX];
+#pragma unroll
+    for (int x = 0; x < KX; x++) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int tile = first; tile < last; tile++) {
-      const int r = tile * 32 + n32;
-      const int limit = r < R ? kv_seen(d, r / G, length, count) : 0;
-      const float fr = factors[row * tiles * 32 + r], ref = r < R ? lse2[row * R + r] : INFINITY;
-      const Frag *qf = frags + ((row * tiles + tile) * PARTS) * KS * 64 + lane;
-      f32x16 s[2];
+      const int r = tile * 16 + n16;
+      const float f_row = fr, z0 = ref;
+      f32x4 s[KX];
 #pragma unroll
-      for (int x = 0; x < 2; x++)
+      for (int x = 0; x < KX; x++) s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 16; e++) s[x][e] = 0.f;
+      for (int k = PARTS * KS - 1; k >= 0; k--)       // (the smaller parts first)
 #pragma unroll
-      for (int pt = PARTS - 1; pt >= 0; pt--)
+        for (int x = 0; x < KX; x++) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x][k % KS].v, next[k].v, s[x], 0, 0, 0);
+      if (tile + 1 < last) load_rows(tile + 1);
 #pragma unroll
-        for (int k = 0; k < KS; k++) {
-          const f16x8 qv = qf[(pt * KS + k) * 64].v;
+      for (int x = 0; x < KX; x++) {
+        const float f = f_row * sk[x];
 #pragma unroll
-          for (int x = 0; x < 2; x++) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x][k].v, qv, s[x], 0, 0, 0);
-        }
-      const bool edge = __any(n0 + 64 > limit);
-#pragma unroll
-      for (int x = 0; x < 2; x++) {
-        const float f = fr * sk[x];
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], f, -ref));
-          acc[x][e] += edge && n0 + 32 * x + (e >> 2) * 8 + hh * 4 + (e & 3) >= limit ? 0.f : p;
-        }
+        for (int e = 0; e < 4; e++) s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], f, -z0));
       }
+      // what the tile's first row sees, the others see
+      if (n0 + kKeysOf > kv_seen(d, tile * 16 / G, length, count) || tile == last - 1) {
+        asm volatile("; masked");                     // (a branch, not selects for every tile)
+        const int limit = r < R ? kv_seen(d, r / G, length, count) : 0;
+#pragma unroll
+        for (int x = 0; x < KX; x++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) s[x][e] = n0 + 16 * x + 4 * g + e < limit ? s[x][e] : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < KX; x++) acc[x] += s[x];
     }
-    // over the 32 rows' lanes; lane 32 x + 8 (e / 4) + 4 hh + e % 4 takes the sum
+    // over the 16 rows' lanes, by way of LDS: a lane then has a key
+    float (&to)[kKeysOf][17] = sums[wave];
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = 0; x < KX; x++)
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        float y = acc[x][e];
-        y += dpp<kDppXor1>(y);
-        y += dpp<kDppXor2>(y);
-        y += dpp<kDppMirror8>(y);
-        y += dpp<kDppMirror16>(y);
-        y = row_swap_sum(y);
-        const float other = __shfl_xor(y, 32);
-        const int at = 32 * x + (e >> 2) * 8 + (e & 3);
-        if (lane == at) sum = hh ? other : y;
-        if (lane == at + 4) sum = hh ? y : other;
-      }
+      for (int e = 0; e < 4; e++) to[16 * x + 4 * g + e][n16] = acc[x][e];
+    __builtin_amdgcn_wave_barrier();                  // (a wave's LDS operations are in order)
+    const int from = lane % kKeysOf;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; i++) part[i % 4] += to[from][i];
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
   }
   const int n = n0 + lane;
-  if (n >= c.capacity || (n >= length && w_in == w_out)) return;
+  if (lane >= kKeysOf || n >= c.capacity || (n >= length && w_in == w_out)) return;
   const int64_t at = row * c.capacity + n;
-  w_out[at] = (w_in ? w_in[at] : 0.f) + (n < length ? sum : 0.f);
+  w_out[at] = (w_in ? w_in[at] : 0.f) + sum;
 }
 
 // ---- host side
@@ -596,14 +548,14 @@ int splits_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
   const int64_t rows = (int64_t)d.heads / c.heads_kv * d.tokens, per = waves_of(c.head_dim) * 32;
   const int64_t wgs = (rows + per - 1) / per * c.heads_kv * c.batch, cus = device_cu_count();
   // as many parts of the keys as fill the chip once, of 512 keys at least
-  return (int)std::max<int64_t>(1, std::min<int64_t>({cus / wgs, (int64_t)c.capacity / 512, 64}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(c.head_dim == 64 ? 2 : 1) * cus / wgs, (int64_t)c.capacity / 512, 64}));
 }
 
 struct Layout { size_t o, ml, lse2, frags, factors, total; int splits; };
 Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
   Layout w;
   w.splits = splits_of(c, d);
-  const size_t rows = (size_t)(d.heads / c.heads_kv) * d.tokens, heads = (size_t)c.batch * c.heads_kv, tiles = (rows + 31) / 32;
+  const size_t rows = (size_t)(d.heads / c.heads_kv) * d.tokens, heads = (size_t)c.batch * c.heads_kv;
   size_t off = 0;
   w.o = off;
   if (w.splits > 1) off += align_up(w.splits * heads * rows * c.head_dim * 4, 256);
@@ -612,16 +564,16 @@ Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
   w.lse2 = off;
   if (weights) off += align_up(heads * rows * 4, 256);
   w.frags = off;
-  if (weights) off += align_up(heads * tiles * 32 * c.head_dim * 2 * (d.dtype == NS_F32 ? 2 : 1), 256);
+  if (weights) off += kv_rows_frag_bytes(c, d);
   w.factors = off;
-  if (weights) off += align_up(heads * tiles * 32 * 4, 256);
+  if (weights) off += kv_rows_factor_bytes(c, d);
   w.total = off;
   return w;
 }
 
 template <typename T, int CODE, int D>
 ns_status launch(const KvAttnArgs &a) {
-  constexpr int WAVES = waves_of(D), PARTS = sizeof(T) == 4 ? 2 : 1, DV = PARTS * D == 512 ? 128 : D;
+  constexpr int WAVES = waves_of(D), DV = sizeof(T) == 4 && D == 256 ? 128 : D;
   const ns_kv_cache &c = a.c;
   const Layout w = layout_of(c, a.d, a.w_out != nullptr);
   const int rows = a.d.heads / c.heads_kv * a.d.tokens, tiles = (rows + WAVES * 32 - 1) / (WAVES * 32);
@@ -644,20 +596,45 @@ ns_status launch(const KvAttnArgs &a) {
   if (st != NS_OK || !a.w_out) return st;
   Frag *frags = reinterpret_cast<Frag *>(a.ws + w.frags);
   float *factors = reinterpret_cast<float *>(a.ws + w.factors);
-  hipLaunchKernelGGL((kv_weights_rows_kernel<T>), dim3((unsigned)((rows + 127) / 128), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256), 0, a.stream, c,
-                     a.d, q, frags, factors);
-  st = check_launch("kv_weights_rows_kernel");
-  if (st != NS_OK) return st;
-  hipLaunchKernelGGL((kv_weights_sum_kernel<PARTS, CODE, D>), dim3((unsigned)((c.capacity + 255) / 256), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256),
-                     0, a.stream, c, a.d, a.lengths, a.counts, frags, factors, p.lse2, a.w_in, a.w_out);
-  return check_launch("kv_weights_sum_kernel");
+  return launch_kv_weights_again(a, frags, factors, p.lse2, true);
 }
 
 template <typename T, int CODE> ns_status launch_d(const KvAttnArgs &a) {
   return a.c.head_dim == 64 ? launch<T, CODE, 64>(a) : a.c.head_dim == 128 ? launch<T, CODE, 128>(a) : launch<T, CODE, 256>(a);
 }
 
+template <int PARTS, int CODE>
+ns_status weights_sum(const KvAttnArgs &a, const Frag *frags, const float *factors, const float *lse2) {
+  const int R = a.d.heads / a.c.heads_kv * a.d.tokens, kx = R > 64 ? 4 : 2;
+  const dim3 grid((unsigned)((a.c.capacity + 64 * kx - 1) / (64 * kx)), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, a.c, a.d, a.lengths, a.counts, frags, factors, lse2, a.w_in, a.w_out);
+    return check_launch("kv_weights_sum_kernel");
+  };
+  if (kx == 4)
+    return a.c.head_dim == 64 ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 4>) : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 4>)
+                                                                                                   : go(kv_weights_sum_kernel<PARTS, CODE, 256, 4>);
+  return a.c.head_dim == 64 ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 2>) : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 2>)
+                                                                                                 : go(kv_weights_sum_kernel<PARTS, CODE, 256, 2>);
+}
+
 }  // namespace
+
+ns_status launch_kv_weights_again(const KvAttnArgs &a, Frag *frags, float *factors, const float *lse2, bool rows) {
+  if (rows) {
+    const int R = a.d.heads / a.c.heads_kv * a.d.tokens;
+    const dim3 grid((unsigned)((R + 63) / 64), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
+    if (a.d.dtype == NS_F32)
+      hipLaunchKernelGGL((kv_weights_rows_kernel<float>), grid, dim3(256), 0, a.stream, a.c, a.d, static_cast<const float *>(a.q), frags, factors);
+    else
+      hipLaunchKernelGGL((kv_weights_rows_kernel<bf16_t>), grid, dim3(256), 0, a.stream, a.c, a.d, static_cast<const bf16_t *>(a.q), frags, factors);
+    const ns_status st = check_launch("kv_weights_rows_kernel");
+    if (st != NS_OK) return st;
+  }
+  if (a.d.dtype == NS_F32)
+    return a.c.code == NS_CODE_I8 ? weights_sum<2, NS_CODE_I8>(a, frags, factors, lse2) : weights_sum<2, NS_CODE_E4M3>(a, frags, factors, lse2);
+  return a.c.code == NS_CODE_I8 ? weights_sum<1, NS_CODE_I8>(a, frags, factors, lse2) : weights_sum<1, NS_CODE_E4M3>(a, frags, factors, lse2);
+}
 
 size_t kv_prompt_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) { return layout_of(c, d, weights).total; }
 
