@@ -42,7 +42,7 @@ struct PromptArgs {
 
 // DV: channels of V, and of out, that a workgroup takes: all, or half of them (fp32, D = 256: registers; the logits are computed twice)
 template <typename T, int CODE, int D, int DV, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
+__global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
                                                                const int32_t *counts, T *out, float *lse, PromptArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = DV / 32, ROWS = WAVES * 32, THREADS = WAVES * 64;
   constexpr uint32_t kV = kKeys * D * 2, kHalf = kV + kKeys * DV * 2;   // bytes of a tile's K, and with its V^T
@@ -397,36 +397,55 @@ __global__ __launch_bounds__(WAVES * 64) void kv_prompt_kernel(ns_kv_cache c, ns
   }
 }
 
-// One wave per row: the splits' results together.
+// The splits' results together: D / 4 threads per row.  The workgroups behind those make the operands of the weights' second pass.
 template <typename T>
-__global__ __launch_bounds__(256) void kv_prompt_join_kernel(ns_kv_cache c, ns_kv_attn_desc d, PromptArgs a, T *out, float *lse) {
-  const int lane = threadIdx.x & 63, D = c.head_dim, G = d.heads / c.heads_kv, R = G * d.tokens;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
+__global__ __launch_bounds__(256) void kv_prompt_join_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, PromptArgs a, T *out, float *lse, Frag *frags,
+                                                             float *factors) {
+  const int tid = threadIdx.x, D = c.head_dim, quads = D / 4, rows = 256 / quads, G = d.heads / c.heads_kv, R = G * d.tokens;
+  const int h = blockIdx.y, b = blockIdx.z, groups = (R + rows - 1) / rows;
+  if ((int)blockIdx.x >= groups) {
+    const int tile = ((int)blockIdx.x - groups) * 4 + (tid >> 6);
+    if (tile < (R + 15) / 16) kv_rows_tile(c, d, q, b, h, tile, tid & 63, frags, factors);
+    return;
+  }
+  const int r = (int)blockIdx.x * rows + tid / quads, dd = tid % quads * 4;
   if (r >= R) return;
   const int64_t heads = (int64_t)c.batch * c.heads_kv, row = (int64_t)b * c.heads_kv + h;
-  float M = -INFINITY;
-  for (int s = 0; s < a.splits; s++) M = fmaxf(M, a.part_ml[((s * heads + row) * R + r) * 2]);
-  const int dd = lane * 4, n = D / 4;                // D = 256: all lanes
+  const float *ml = a.part_ml + (row * R + r) * 2, *o = a.part_o + (row * R + r) * D + dd;
+  const int64_t apart = heads * R;                  // records between two splits'
+  float M = -INFINITY, L = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.f;
-  for (int s = 0; s < a.splits; s++) {
-    const int64_t rec = (s * heads + row) * R + r;
-    const float ms = a.part_ml[rec * 2];
-    if (ms == -INFINITY) continue;
-    const float fade = __builtin_amdgcn_exp2f(ms - M);
-    L += a.part_ml[rec * 2 + 1] * fade;
-    if (lane < n) y += *reinterpret_cast<const f32x4 *>(a.part_o + rec * D + dd) * fade;
+  for (int s0 = 0; s0 < a.splits; s0 += 4) {        // (four records on their way at a time)
+    f32x2 z[4];
+    f32x4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int64_t s = min(s0 + i, a.splits - 1);
+      z[i] = *reinterpret_cast<const f32x2 *>(ml + s * apart * 2);
+      v[i] = *reinterpret_cast<const f32x4 *>(o + s * apart * D);
+    }
+    float next = M;
+#pragma unroll
+    for (int i = 0; i < 4; i++) next = fmaxf(next, s0 + i < a.splits ? z[i][0] : -INFINITY);
+    const float ref = next == -INFINITY ? 0.f : next, keep = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - ref);
+    y *= keep;
+    L *= keep;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      if (s0 + i < a.splits && z[i][0] != -INFINITY) {
+        const float fade = __builtin_amdgcn_exp2f(z[i][0] - ref);
+        y += v[i] * fade;
+        L += z[i][1] * fade;
+      }
+    M = next;
   }
   const bool some = M != -INFINITY;
   const int t = r / G, hq = h * G + r - t * G;
-  if (lane < n) {
-    const float inv = some ? 1.f / L : 0.f;
+  const float inv = some ? 1.f / L : 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; j++) y[j] = some ? y[j] * inv : 0.f;
-    T *p = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd;
-    store4(p, y);
-  }
-  if (lane == 0) {
+  for (int j = 0; j < 4; j++) y[j] = some ? y[j] * inv : 0.f;
+  store4(out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + dd, y);
+  if (dd == 0) {
     const float z2 = some ? M + __log2f(L) : -INFINITY;
     if (lse) lse[((int64_t)b * d.heads + hq) * d.tokens + t] = z2 * kLn2;
     if (a.lse2) a.lse2[row * R + r] = some ? z2 : INFINITY;
@@ -460,6 +479,9 @@ __global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_k
   // causal: the first row that sees key n0 is that of the query at its position
   const int first = d.causal ? (int)min((int64_t)max(0, n0 - (length - count)) * G / 16, (int64_t)tiles) : 0;
   const int last = min(tiles, (count * G + 15) / 16);
+  // from here on a tile's rows see all these keys (but for the last tile's, some of which may be no rows)
+  const int query = n0 + kKeysOf - 1 - (length - count);              // the one at the last key's position
+  const int clear = n0 + kKeysOf > length ? tiles : d.causal ? (int)min(((int64_t)max(0, query) * G + 15) / 16, (int64_t)tiles) : 0;
   if (n0 < length && first < last) {
     const uint8_t *kp = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h + (int64_t)n0 * c.stride_t;
     const uint32_t off = (uint32_t)n16 * (uint32_t)c.stride_t + 16 * g;
@@ -509,8 +531,7 @@ __global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_k
 #pragma unroll
         for (int e = 0; e < 4; e++) s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], f, -z0));
       }
-      // what the tile's first row sees, the others see
-      if (n0 + kKeysOf > kv_seen(d, tile * 16 / G, length, count) || tile == last - 1) {
+      if (tile < clear || tile == last - 1) {
         asm volatile("; masked");                     // (a branch, not selects for every tile)
         const int limit = r < R ? kv_seen(d, r / G, length, count) : 0;
 #pragma unroll
@@ -548,7 +569,7 @@ int splits_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
   const int64_t rows = (int64_t)d.heads / c.heads_kv * d.tokens, per = waves_of(c.head_dim) * 32;
   const int64_t wgs = (rows + per - 1) / per * c.heads_kv * c.batch, cus = device_cu_count();
   // as many parts of the keys as fill the chip once, of 512 keys at least
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(c.head_dim == 64 ? 2 : 1) * cus / wgs, (int64_t)c.capacity / 512, 64}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(c.head_dim == 64 ? 3 : 1) * cus / wgs, (int64_t)c.capacity / 512, 64}));
 }
 
 struct Layout { size_t o, ml, lse2, frags, factors, total; int splits; };
@@ -588,15 +609,16 @@ ns_status launch(const KvAttnArgs &a) {
   const dim3 grid((unsigned)((int64_t)tiles * w.splits * (D / DV) * c.heads_kv * c.batch));
   hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES>), grid, dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out, a.lse, p);
   st = check_launch("kv_prompt_kernel");
+  Frag *frags = reinterpret_cast<Frag *>(a.ws + w.frags);
+  float *factors = reinterpret_cast<float *>(a.ws + w.factors);
   if (st == NS_OK && w.splits > 1) {
-    hipLaunchKernelGGL((kv_prompt_join_kernel<T>), dim3((unsigned)((rows + 3) / 4), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256), 0, a.stream, c, a.d,
-                       p, out, a.lse);
+    const int per = 1024 / D, more = a.w_out ? (rows + 63) / 64 : 0;
+    hipLaunchKernelGGL((kv_prompt_join_kernel<T>), dim3((unsigned)((rows + per - 1) / per + more), (unsigned)c.heads_kv, (unsigned)c.batch), dim3(256), 0,
+                       a.stream, c, a.d, q, p, out, a.lse, frags, factors);
     st = check_launch("kv_prompt_join_kernel");
   }
   if (st != NS_OK || !a.w_out) return st;
-  Frag *frags = reinterpret_cast<Frag *>(a.ws + w.frags);
-  float *factors = reinterpret_cast<float *>(a.ws + w.factors);
-  return launch_kv_weights_again(a, frags, factors, p.lse2, true);
+  return launch_kv_weights_again(a, frags, factors, p.lse2, w.splits == 1);
 }
 
 template <typename T, int CODE> ns_status launch_d(const KvAttnArgs &a) {
