@@ -461,10 +461,9 @@ __global__ __launch_bounds__(256) void kv_weights_rows_kernel(ns_kv_cache c, ns_
   if (tile < (R + 15) / 16) kv_rows_tile(c, d, q, blockIdx.z, blockIdx.y, tile, threadIdx.x & 63, frags, factors);
 }
 
-// KX: tiles of 16 keys that a wave has: four for many rows (an operand of theirs serves all), two for few (more waves, more loads on
-// their way)
+// Many rows: a wave's keys stay, the rows' operands come from the L2, an operand serves KX tiles of 16 keys.
 template <int PARTS, int CODE, int D, int KX>
-__global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
+__global__ __launch_bounds__(256, 2) void kv_weights_sum_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
                                                              const Frag *frags, const float *factors, const float *lse2, const float *w_in,
                                                              float *w_out) {
   constexpr int KS = D / 32, kKeysOf = 16 * KX;
@@ -503,7 +502,7 @@ __global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_k
       for (int k = 0; k < PARTS * KS; k++) next[k] = qp[((int64_t)tile * PARTS * KS + k) * 64];
       const int r = tile * 16 + n16;
       fr = factors[row * tiles * 16 + r];
-      ref = r < R ? lse2[row * R + r] : INFINITY;
+      ref = lse2[row * R + min(r, R - 1)];            // (rows that are none are masked)
     };
     load_rows(first);
     Frag kf[KX][KS];
@@ -559,6 +558,98 @@ __global__ __launch_bounds__(256) void kv_weights_sum_kernel(ns_kv_cache c, ns_k
   if (lane >= kKeysOf || n >= c.capacity || (n >= length && w_in == w_out)) return;
   const int64_t at = row * c.capacity + n;
   w_out[at] = (w_in ? w_in[at] : 0.f) + sum;
+}
+
+// Few rows: the operands of QT tiles of them stay in registers, and a wave takes `steps` times 32 keys, the next ones' codes on their way.
+template <int PARTS, int CODE, int D, int QT>
+__global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
+                                                                   const Frag *frags, const float *factors, const float *lse2, const float *w_in,
+                                                                   float *w_out, int steps) {
+  constexpr int KS = D / 32, KX = 2, kKeysOf = 16 * KX;
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 15) / 16, lblock = 31 - __clz(c.block);
+  const int h = blockIdx.y, b = blockIdx.z;
+  __shared__ float sums[4][kKeysOf][17];
+  const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
+  const int64_t row = (int64_t)b * c.heads_kv + h;
+  int n0 = ((int)blockIdx.x * steps * 4 + wave) * kKeysOf;
+  const int end = min(n0 + steps * 4 * kKeysOf, c.capacity), seen = w_in == w_out ? min(end, length) : end;
+  if (n0 >= seen) return;
+
+  const uint8_t *kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
+  const uint32_t off = (uint32_t)n16 * (uint32_t)c.stride_t + 16 * g;
+  u32x4 kw[KX][D / 64];
+  float next_sk;
+  auto fetch = [&](int n) {
+    const uint8_t *kp = kb + (int64_t)n * c.stride_t;
+    const uint32_t o = (uint32_t)opaque((int)off);
+#pragma unroll
+    for (int x = 0; x < KX; x++)
+#pragma unroll
+      for (int i = 0; i < D / 64; i++) kw[x][i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)16 * x * c.stride_t + 64 * i + o);
+    next_sk = c.k_scale[row * (c.capacity >> lblock) + (n >> lblock)];
+  };
+  if (n0 < length) fetch(n0);
+  Frag qf[QT][PARTS * KS];
+  float fr[QT], ref[QT];
+  int limit[QT];
+#pragma unroll
+  for (int t = 0; t < QT; t++) {
+    const int tile = min(t, tiles - 1), r = t * 16 + n16;
+    const Frag *qp = frags + ((row * tiles + tile) * PARTS) * KS * 64 + lane;
+#pragma unroll
+    for (int k = 0; k < PARTS * KS; k++) qf[t][k] = qp[k * 64];
+    limit[t] = r < R ? kv_seen(d, r / G, length, count) : 0;
+    fr[t] = factors[row * tiles * 16 + tile * 16 + n16];
+    ref[t] = lse2[row * R + min(r, R - 1)];
+  }
+  for (; n0 < seen; n0 += 4 * kKeysOf) {
+    f32x4 acc[KX];
+#pragma unroll
+    for (int x = 0; x < KX; x++) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (n0 < length) {
+      Frag kf[KX][KS];
+#pragma unroll
+      for (int x = 0; x < KX; x++)
+#pragma unroll
+        for (int k = 0; k < KS; k++) kf[x][k] = kv_frag<CODE>(kw[x][k / 2][2 * (k % 2)], kw[x][k / 2][2 * (k % 2) + 1]);
+      const float sk = next_sk;
+      if (n0 + 4 * kKeysOf < min(end, length)) fetch(n0 + 4 * kKeysOf);
+#pragma unroll
+      for (int t = 0; t < QT; t++) {
+        const float f = fr[t] * sk;
+#pragma unroll
+        for (int x = 0; x < KX; x++) {
+          f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = PARTS * KS - 1; k >= 0; k--) s = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x][k % KS].v, qf[t][k].v, s, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], f, -ref[t]));
+            acc[x][e] += n0 + 16 * x + 4 * g + e < limit[t] ? p : 0.f;
+          }
+        }
+      }
+    }
+    // over the 16 rows' lanes, by way of LDS: a lane then has a key
+    float (&to)[kKeysOf][17] = sums[wave];
+    __builtin_amdgcn_wave_barrier();                  // (a wave's LDS operations are in order)
+#pragma unroll
+    for (int x = 0; x < KX; x++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) to[16 * x + 4 * g + e][n16] = acc[x][e];
+    __builtin_amdgcn_wave_barrier();
+    const int key = lane % kKeysOf, part = lane / kKeysOf * 8;        // two lanes a key, eight rows each
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) sum += to[key][part + i];
+    sum = half_swap_sum(sum);
+    const int n = n0 + key;
+    if (lane < kKeysOf && n < seen) {
+      const int64_t at = row * c.capacity + n;
+      w_out[at] = (w_in ? w_in[at] : 0.f) + sum;
+    }
+  }
 }
 
 // ---- host side
@@ -627,17 +718,33 @@ template <typename T, int CODE> ns_status launch_d(const KvAttnArgs &a) {
 
 template <int PARTS, int CODE>
 ns_status weights_sum(const KvAttnArgs &a, const Frag *frags, const float *factors, const float *lse2) {
-  const int R = a.d.heads / a.c.heads_kv * a.d.tokens, kx = R > 64 ? 4 : 2;
-  const dim3 grid((unsigned)((a.c.capacity + 64 * kx - 1) / (64 * kx)), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
+  const int R = a.d.heads / a.c.heads_kv * a.d.tokens;
+  // registers for the operands of that many tiles of rows (64 of them), or 64 keys a wave
+  const int tiles = R <= 32 ? 2 : R <= 64 ? 4 : 1 << 20;
+  if (tiles * PARTS * a.c.head_dim <= 512) {
+    // steps of 32 keys a wave: so many that all waves are on the chip at once, eight at most
+    const int64_t pieces = (int64_t)(a.c.capacity / 32) * a.c.heads_kv * a.c.batch;
+    const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(8, pieces / ((int64_t)device_cu_count() * 16)));
+    const dim3 grid((unsigned)((a.c.capacity + 128 * steps - 1) / (128 * steps)), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, a.c, a.d, a.lengths, a.counts, frags, factors, lse2, a.w_in, a.w_out, steps);
+      return check_launch("kv_weights_stream_kernel");
+    };
+    if (a.c.head_dim == 64) return tiles == 2 ? go(kv_weights_stream_kernel<PARTS, CODE, 64, 2>) : go(kv_weights_stream_kernel<PARTS, CODE, 64, 4>);
+    if constexpr (PARTS == 1) {
+      if (a.c.head_dim == 256) return go(kv_weights_stream_kernel<PARTS, CODE, 256, 2>);
+      if (tiles == 4) return go(kv_weights_stream_kernel<PARTS, CODE, 128, 4>);
+    }
+    return go(kv_weights_stream_kernel<PARTS, CODE, 128, 2>);
+  }
+  const int keys = PARTS * a.c.head_dim == 512 ? 128 : 256;            // of a workgroup
+  const dim3 grid((unsigned)((a.c.capacity + keys - 1) / keys), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, a.c, a.d, a.lengths, a.counts, frags, factors, lse2, a.w_in, a.w_out);
     return check_launch("kv_weights_sum_kernel");
   };
-  if (kx == 4)
-    return a.c.head_dim == 64 ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 4>) : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 4>)
-                                                                                                   : go(kv_weights_sum_kernel<PARTS, CODE, 256, 4>);
-  return a.c.head_dim == 64 ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 2>) : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 2>)
-                                                                                                 : go(kv_weights_sum_kernel<PARTS, CODE, 256, 2>);
+  return a.c.head_dim == 64 ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 4>) : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 4>)
+                                                                                                 : go(kv_weights_sum_kernel<PARTS, CODE, 256, PARTS == 2 ? 2 : 4>);
 }
 
 }  // namespace
