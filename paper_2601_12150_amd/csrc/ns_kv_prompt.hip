@@ -579,8 +579,10 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
   const uint8_t *kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
   const uint32_t off = (uint32_t)n16 * (uint32_t)c.stride_t + 16 * g;
   u32x4 kw[KX][D / 64];
-  float next_sk;
+  float next_sk, next_w = 0.f;
   auto fetch = [&](int n) {
+    if (w_in && n + lane % kKeysOf < seen) next_w = w_in[row * c.capacity + n + lane % kKeysOf];
+    if (n >= length) return;
     const uint8_t *kp = kb + (int64_t)n * c.stride_t;
     const uint32_t o = (uint32_t)opaque((int)off);
 #pragma unroll
@@ -589,7 +591,7 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
       for (int i = 0; i < D / 64; i++) kw[x][i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)16 * x * c.stride_t + 64 * i + o);
     next_sk = c.k_scale[row * (c.capacity >> lblock) + (n >> lblock)];
   };
-  if (n0 < length) fetch(n0);
+  fetch(n0);
   Frag qf[QT][PARTS * KS];
   float fr[QT], ref[QT];
   int limit[QT];
@@ -607,6 +609,7 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
     f32x4 acc[KX];
 #pragma unroll
     for (int x = 0; x < KX; x++) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float before = next_w;
     if (n0 < length) {
       Frag kf[KX][KS];
 #pragma unroll
@@ -614,7 +617,7 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
 #pragma unroll
         for (int k = 0; k < KS; k++) kf[x][k] = kv_frag<CODE>(kw[x][k / 2][2 * (k % 2)], kw[x][k / 2][2 * (k % 2) + 1]);
       const float sk = next_sk;
-      if (n0 + 4 * kKeysOf < min(end, length)) fetch(n0 + 4 * kKeysOf);
+      if (n0 + 4 * kKeysOf < seen) fetch(n0 + 4 * kKeysOf);
 #pragma unroll
       for (int t = 0; t < QT; t++) {
         const float f = fr[t] * sk;
@@ -630,6 +633,8 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
           }
         }
       }
+    } else if (n0 + 4 * kKeysOf < seen) {
+      fetch(n0 + 4 * kKeysOf);
     }
     // over the 16 rows' lanes, by way of LDS: a lane then has a key
     float (&to)[kKeysOf][17] = sums[wave];
@@ -645,10 +650,7 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
     for (int i = 0; i < 8; i++) sum += to[key][part + i];
     sum = half_swap_sum(sum);
     const int n = n0 + key;
-    if (lane < kKeysOf && n < seen) {
-      const int64_t at = row * c.capacity + n;
-      w_out[at] = (w_in ? w_in[at] : 0.f) + sum;
-    }
+    if (lane < kKeysOf && n < seen) w_out[row * c.capacity + n] = before + sum;
   }
 }
 
@@ -722,9 +724,9 @@ ns_status weights_sum(const KvAttnArgs &a, const Frag *frags, const float *facto
   // registers for the operands of that many tiles of rows (64 of them), or 64 keys a wave
   const int tiles = R <= 32 ? 2 : R <= 64 ? 4 : 1 << 20;
   if (tiles * PARTS * a.c.head_dim <= 512) {
-    // steps of 32 keys a wave: so many that all waves are on the chip at once, eight at most
+    // steps of 32 keys a wave: so many that all waves are on the chip at once, four at most
     const int64_t pieces = (int64_t)(a.c.capacity / 32) * a.c.heads_kv * a.c.batch;
-    const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(8, pieces / ((int64_t)device_cu_count() * 16)));
+    const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(4, pieces / ((int64_t)device_cu_count() * 16)));
     const dim3 grid((unsigned)((a.c.capacity + 128 * steps - 1) / (128 * steps)), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
     auto go = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, a.c, a.d, a.lengths, a.counts, frags, factors, lse2, a.w_in, a.w_out, steps);
