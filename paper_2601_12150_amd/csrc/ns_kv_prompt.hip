@@ -133,6 +133,7 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
   const int lblock = 31 - __clz(c.block);
   constexpr int KP = kKeys * D / 16 / THREADS, VP = kKeys / 4 * (DV / 4) / THREADS;      // pieces a thread has of K (16 codes) and V (4 x 4)
   constexpr int KR = THREADS / (D / 16), VR = THREADS / (DV / 4) * 4;                    // keys between two of its pieces
+  static_assert((KP == 1 || (KR <= 32 && 32 % KR == 0)) && (VP == 1 || (VR <= 32 && 32 % VR == 0)), "key 32 begins a piece of all threads");
   const int k_key = tid / (D / 16), v_key = tid / (DV / 4) * 4;
   const uint32_t stride = (uint32_t)c.stride_t, k_off = (uint32_t)k_key * stride + tid % (D / 16) * 16, v_off = (uint32_t)v_key * stride + tid % (DV / 4) * 4;
   u32x4 kraw[KP];
@@ -145,16 +146,18 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
     next_vs[0] = vs[n0 >> lblock];
     next_vs[1] = vs[n1 >> lblock];
     const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
-    // (the last tile of blocks of 32 may reach 32 keys beyond the capacity: their places take the 32 before once more)
+    // (the last tile of blocks of 32 may reach 32 keys beyond the capacity: their places take the 32 before once more.  Where a thread has
+    // several pieces the first ones of all threads are before key 32, and whole pieces lie behind it)
     const uint32_t back = n0 + kKeys > c.capacity ? 32 * stride : 0u;
+    const uint32_t k_from = k_off - (KP == 1 && k_key >= 32 ? back : 0u), v_from = v_off - (VP == 1 && v_key >= 32 ? back : 0u);
 #pragma unroll
     for (int i = 0; i < KP; i++)
-      kraw[i] = *reinterpret_cast<const u32x4 *>(kp + (int64_t)i * KR * c.stride_t + (k_off - (k_key + i * KR >= 32 ? back : 0u)));
+      kraw[i] = *reinterpret_cast<const u32x4 *>(kp + ((int64_t)i * KR * c.stride_t - (i * KR >= 32 ? back : 0u)) + k_from);
 #pragma unroll
     for (int i = 0; i < VP; i++)
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        vraw[i][j] = *reinterpret_cast<const uint32_t *>(vp + (int64_t)(i * VR + j) * c.stride_t + (v_off - (v_key + i * VR >= 32 ? back : 0u)));
+        vraw[i][j] = *reinterpret_cast<const uint32_t *>(vp + ((int64_t)(i * VR + j) * c.stride_t - (i * VR >= 32 ? back : 0u)) + v_from);
   };
   // V's scales: o is in units of `unit`, a tile's V in LDS in units of `next`, which is the same but where a much larger scale
   // comes along.  Where both halves' scales are next times a plain ratio, V is multiplied by that on its way (slow = false); else (a NaN, far

@@ -302,6 +302,50 @@ def test_attention_of_queries_of_any_size(nb, T, size):
         check_attention(*got, oracle.attend(q, k, v, [N], [T], scale, True), dtype, D, N, 2 * T)
 
 
+@pytest.mark.parametrize("code,dtype,D,G,T", [
+    ("i8", "bf16", 64, 1, 1), ("e4m3", "f32", 128, 4, 4), ("i8", "bf16", 64, 2, 300), ("e4m3", "bf16", 128, 2, 200), ("i8", "bf16", 128, 4, 200),
+    ("e4m3", "f32", 64, 1, 150), ("i8", "f32", 128, 1, 150), ("e4m3", "bf16", 256, 1, 90), ("i8", "f32", 256, 2, 90)])
+@pytest.mark.parametrize("kind", ["near", "far", "own"])
+def test_attention_of_blocks_of_different_sizes(nb, code, dtype, D, G, T, kind):
+    """Values whose blocks' scales are a little and far apart (2^-60 .. 2^40), or no powers of two; blocks of zeros, the first one and
+    others; and K's blocks of different sizes.  A row that sees only small blocks is not the worse for larger ones behind."""
+    B, H, block, N = 2, 2, 32, 608
+    rng = np.random.default_rng(D + T)
+    cache, host = make(nb, rng, B, H, N, D, block, code, [N, 333])
+    n = N // block
+    scale = {"near": np.exp2(rng.integers(-12, 6, (B, H, n)).astype(np.float64)), "far": np.exp2(rng.integers(-60, 41, (B, H, n)).astype(np.float64)),
+             "own": rng.uniform(0.001, 1, (B, H, n))}[kind]
+    for j in (0, 5, 6, 11):
+        host[2][:, :, j * block:(j + 1) * block] = 0.0
+        scale[:, :, j] = 2.0 ** -100
+    v, vs = torch.from_numpy(host[2]).float().to(CODES[code]).cuda(), dev(scale, torch.float32)
+    ks = dev(rng.uniform(0.002, 0.02, (B, H, n)), torch.float32)
+    cache = nb.kv_cache(cache.k, v, ks, vs)
+    key, value = oracle.values(host[0], f64(ks)), oracle.values(host[2], f64(vs))
+    q = rounded((rng.standard_normal((B, H * G, T, D)) / np.abs(key).mean()).astype(np.float32), dtype)
+    got = nb.kv_cache_attn(cache, dev(q, DTYPES[dtype]), i32([N, 333]), want_lse=True, want_weights=True)
+    scale = float(np.float32(D ** -0.5))
+    check_attention(*got, oracle.attend(q, key, value, [N, 333], [T] * B, scale, True), dtype, D, N, G * T)
+
+
+@pytest.mark.parametrize("dtype,code,B,H,G,D,block,N,T,padded", [
+    ("bf16", "i8", 150, 2, 8, 64, 64, 2048, 3, False),             # 24 rows of many sequences: shares of the keys that cross them
+    ("bf16", "e4m3", 129, 2, 1, 128, 128, 4096, 1, False),         # a workgroup per sequence and head
+    ("f32", "i8", 40, 8, 2, 64, 32, 320, 150, True),               # more tiles of rows than the chip takes at once
+    ("bf16", "i8", 48, 8, 2, 64, 32, 320, 150, True),
+    ("bf16", "e4m3", 40, 8, 2, 128, 64, 320, 150, True),
+    ("f32", "e4m3", 30, 8, 2, 128, 64, 320, 150, True),
+    ("bf16", "i8", 24, 8, 2, 256, 128, 256, 130, True),
+    ("f32", "i8", 20, 4, 2, 256, 64, 256, 130, True),
+])
+def test_attention_of_many_sequences(nb, dtype, code, B, H, G, D, block, N, T, padded):
+    rng = np.random.default_rng(B)
+    lengths = [int(n) for n in rng.integers(0, N + 1, B)]
+    lengths[:4] = [N, 0, 1, T]
+    counts = [int(n) for n in rng.integers(0, T + 1, B)] if padded else None
+    attention_case(nb, dtype, code, B, H, G, D, block, N, T, lengths, counts)
+
+
 @pytest.mark.parametrize("T", [1, 70])
 def test_attention_of_nan(nb, T):
     """A NaN block makes the rows that see it NaN and no other; a NaN query its own row."""
@@ -406,6 +450,21 @@ def test_evict_of_long_sequences(nb, length):
         ref, ref_scale = oracle.move(host[0][0, h], host[1][0, h], want, block, "e4m3")
         assert np.array_equal(f64(to.k[0, h]), ref) and np.array_equal(f64(to.k_scale[0, h]), ref_scale)
         assert np.array_equal(kept[1, h, :1000], np.arange(1000)) and (kept[1, h, 1000:] == -1).all()
+
+
+def test_evict_of_a_long_sequence_with_nothing_to_rank(nb):
+    """The first and the last tokens of more than 32768, and no others, stay."""
+    rng = np.random.default_rng(5)
+    N, n = 40000 // 32 * 32 + 32, 40000
+    cache, host = make(nb, rng, 1, 1, N, 64, 32, "i8", [n], poison=False)
+    to = nb.kv_cache_empty(1, 1, 320, 64, 32)
+    w = dev(evict_weights(rng, (1, 1, N), "odd"))
+    kept, w_out, left = nb.kv_cache_evict(cache, to, w, i32([n]), 300, n_global=100, n_recent=200)
+    want = np.concatenate([np.arange(100), np.arange(n - 200, n)])
+    assert np.array_equal(kept.cpu().numpy()[0, 0], want) and left.tolist() == [300]
+    assert np.array_equal(w_out.cpu().numpy()[0, 0, :300], w.cpu().numpy()[0, 0, want], equal_nan=True)
+    ref, ref_scale = oracle.move(host[2][0, 0], host[3][0, 0], want, 32, "i8")
+    assert np.array_equal(f64(to.v[0, 0]), ref) and np.array_equal(f64(to.v_scale[0, 0]), ref_scale)
 
 
 def test_evict_of_nan_blocks(nb):
@@ -598,6 +657,43 @@ def test_graph_replays_match_eager(nb):
         torch.cuda.synchronize()
         for a, b in zip(want, static):
             assert torch.equal(a.view(torch.uint8) if a.element_size() == 1 else a, b.view(torch.uint8) if b.element_size() == 1 else b), "replay %d" % r
+
+
+@pytest.mark.parametrize("B,H,G,D,T", [(40, 8, 2, 128, 150), (2, 2, 4, 64, 70)])
+def test_graphs_of_prompts_that_share_a_workspace(nb, B, H, G, D, T):
+    """Two graphs of prompts with weights, recorded with one workspace between them and replayed in turn with new lengths and queries."""
+    import ctypes
+    N, block = 320, 64
+    rng = np.random.default_rng(12)
+    cache, _ = make(nb, rng, B, H, N, D, block, "i8", [N] * B)
+    c = nb.ns_kv_cache(B, H, D, N, block, nb.NS_CODE_I8, *cache.k.stride()[:3], *(t.data_ptr() for t in cache))
+    q, lengths = torch.zeros((B, H * G, T, D), device="cuda", dtype=torch.bfloat16), i32([0] * B)
+    d = nb.ns_kv_attn_desc(H * G, T, nb.NS_BF16, 1, D ** -0.5, *q.stride()[:3], *q.stride()[:3])
+    ws = torch.full((nb.lib.kv_cache_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(d), 1),), 0xff, device="cuda", dtype=torch.uint8)
+    outs = [[torch.zeros_like(q), torch.zeros((B, H, N), device="cuda")] for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        nb.kv_cache_attn(cache, q, lengths, out=outs[0][0], weights_out=outs[0][1], workspace=ws)
+    torch.cuda.synchronize()
+    graphs = []
+    for i, causal in enumerate((True, False)):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            nb.kv_cache_attn(cache, q, lengths, causal=causal, out=outs[i][0], weights_out=outs[i][1], workspace=ws)
+        graphs.append(graph)
+    for r in range(4):
+        q.normal_()
+        lengths.copy_(i32(rng.integers(0, N + 1, B).tolist()))
+        torch.cuda.synchronize()
+        for i in (0, 1, 0):
+            outs[i][0].fill_(7), outs[i][1].fill_(7)
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for i, causal in enumerate((True, False)):
+            want = nb.kv_cache_attn(cache, q, lengths, causal=causal, want_weights=True)
+            there = (torch.arange(N, device="cuda") < lengths[:, None, None]).expand(B, H, N)
+            assert torch.equal(outs[i][0], want[0]) and torch.equal(outs[i][1][there], want[1][there]), "replay %d" % r
 
 
 def test_calls_on_two_streams(nb):
