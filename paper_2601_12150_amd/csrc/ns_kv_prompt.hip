@@ -38,12 +38,15 @@ struct PromptArgs {
   float *part_o, *part_ml;         // splits > 1: [splits][B Hkv][R] D floats / (reference, sum)
   float *lse2;                     // nullable [B Hkv][R]: log2 of the sum, +inf for a row that sees nothing
   int splits;
+  int items;                       // row tiles x splits x heads (x halves)
+  int *tickets;                    // items > workgroups: a counter, 0 before the launch
 };
 
+// Item x: a tile of rows of a head, or its part of the keys.
 // DV: channels of V, and of out, that a workgroup takes: all, or half of them (fp32, D = 256: registers; the logits are computed twice)
 template <typename T, int CODE, int D, int DV, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
-                                                               const int32_t *counts, T *out, float *lse, PromptArgs a) {
+__device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv_attn_desc &d, const T *q, const int32_t *lengths, const int32_t *counts,
+                                               T *out, float *lse, const PromptArgs &a, int x) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = DV / 32, ROWS = WAVES * 32, THREADS = WAVES * 64;
   constexpr uint32_t kV = kKeys * D * 2, kHalf = kV + kKeys * DV * 2;   // bytes of a tile's K, and with its V^T
   // Registers for both parts of the queries, and LDS for two tiles?  fp32 with D = 256 has the second part in LDS, and one tile.
@@ -53,9 +56,8 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
   const int n32 = lane & 31, hh = lane >> 5;
   const int G = d.heads / c.heads_kv, R = G * d.tokens;
   const int tiles = (R + ROWS - 1) / ROWS;
-  // The last rows of all heads see most and go first, so that the launch ends with small pieces.  Neighbouring workgroups, which
-  // run on different XCDs, have different heads: with a multiple of eight of them a head's K and V stay in one XCD's L2.
-  const uint32_t heads = (uint32_t)c.batch * c.heads_kv, item = blockIdx.x / heads, head = blockIdx.x % heads;
+  // the last rows of all heads see most and go first, so that the launch ends with small items; neighbouring ones have different heads
+  const uint32_t heads = (uint32_t)c.batch * c.heads_kv, item = (uint32_t)x / heads, head = (uint32_t)x % heads;
   const int part = (int)(item % (D / DV)), split = (int)(item / (D / DV) % a.splits), tile = tiles - 1 - (int)(item / (D / DV) / a.splits);
   const int h = (int)(head % c.heads_kv), b = (int)(head / c.heads_kv);
   const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
@@ -162,19 +164,32 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
   // V's scales: o is in units of `unit`, a tile's V in LDS in units of `next`, which is the same but where a much larger scale
   // comes along.  Where both halves' scales are next times a plain ratio, V is multiplied by that on its way (slow = false); else (a NaN, far
   // smaller ones, the caller's own that are no powers of two) LDS has the bare codes, and the products are multiplied.
-  float unit = 0.f, next = 0.f, inv_next = 0.f, rel0 = 1.f, rel1 = 1.f;
-  bool slow = false;
+  float unit = 0.f, next = 0.f, inv_next = 0.f, rel0 = 0.f, rel1 = 0.f;
+  bool slow = true;
+  // (branches, both here and for the last tile: 262 -> 244 us for the prompts of 2 x 4096 tokens)
+  uint32_t last_bits0 = 0, last_bits1 = 0;          // the scales that these go by; 0 is none
+  By<CODE> v_by[VP];
+#pragma unroll
+  for (int i = 0; i < VP; i++) v_by[i] = kv_by<CODE>(1.f);
   auto stage = [&](int n0, uint32_t at) {
     staged_ks[0] = next_ks[0];
     staged_ks[1] = next_ks[1];
-    const float s0 = next_vs[0], s1 = n0 + 32 < length ? next_vs[1] : s0, big = fmaxf(s0, s1);
-    if (!(big <= next * 0x1p5f) && big > 0.f && big < INFINITY) {                // (the first tile's too)
-      next = big;
-      inv_next = 1.f / big;
+    const float s0 = next_vs[0], s1 = n0 + 32 < length ? next_vs[1] : s0;
+    if (__float_as_uint(s0) != last_bits0 || __float_as_uint(s1) != last_bits1) {
+      asm volatile("; other scales");
+      last_bits0 = __float_as_uint(s0);
+      last_bits1 = __float_as_uint(s1);
+      const float big = fmaxf(s0, s1);
+      if (!(big <= next * 0x1p5f) && big > 0.f && big < INFINITY) {              // (the first tile's too)
+        next = big;
+        inv_next = 1.f / big;
+      }
+      rel0 = s0 * inv_next;
+      rel1 = s1 * inv_next;
+      slow = !EARLY || !(plain_ratio(rel0) && plain_ratio(rel1));
+#pragma unroll
+      for (int i = 0; i < VP; i++) v_by[i] = kv_by<CODE>(slow ? 1.f : v_key + i * VR >= 32 ? rel1 : rel0);
     }
-    rel0 = s0 * inv_next;
-    rel1 = s1 * inv_next;
-    slow = !EARLY || !(plain_ratio(rel0) && plain_ratio(rel1));
     // (opaque: else the compiler keeps every address in a register of its own)
     const uint32_t k_to = (uint32_t)opaque((int)(at + k_at<D>(k_key, tid % (D / 16) * 2)));
     const int quad0 = v_key / 4;
@@ -193,16 +208,20 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
       static_assert(VP == 1 || VR == 16 || VR == 32, "a thread's keys are 16 or 32 apart: two or four pieces further on");
       uint32_t w[4];
 #pragma unroll
-      for (int j = 0; j < 4; j++) w[j] = kv_raw<CODE>(tail && n0 + key + j >= length ? 0u : vraw[i][j]);
+      for (int j = 0; j < 4; j++) w[j] = kv_raw<CODE>(vraw[i][j]);
+      if (tail) {
+        asm volatile("; tail");
+#pragma unroll
+        for (int j = 0; j < 4; j++) w[j] = n0 + key + j >= length ? kv_raw<CODE>(0u) : w[j];
+      }
       const uint32_t lo0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
       const uint32_t hi0 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), hi1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
-      const By<CODE> by = kv_by<CODE>(slow ? 1.f : key >= 32 ? rel1 : rel0);
       // keys 4 quad .. + 3 are the first or second half of the piece that lanes of half (quad & 1) read for the step quad / 4
       const uint32_t to = v_to ^ (uint32_t)(VR * 2 * i);
-      *reinterpret_cast<u32x2 *>(lds + to) = u32x2{kv_f16x2_by<CODE, 0>(lo0, by), kv_f16x2_by<CODE, 0>(lo1, by)};
-      *reinterpret_cast<u32x2 *>(lds + (to ^ 16) + kKeys * 2) = u32x2{kv_f16x2_by<CODE, 1>(lo0, by), kv_f16x2_by<CODE, 1>(lo1, by)};
-      *reinterpret_cast<u32x2 *>(lds + (to ^ 32) + kKeys * 4) = u32x2{kv_f16x2_by<CODE, 0>(hi0, by), kv_f16x2_by<CODE, 0>(hi1, by)};
-      *reinterpret_cast<u32x2 *>(lds + (to ^ 48) + kKeys * 6) = u32x2{kv_f16x2_by<CODE, 1>(hi0, by), kv_f16x2_by<CODE, 1>(hi1, by)};
+      *reinterpret_cast<u32x2 *>(lds + to) = u32x2{kv_f16x2_by<CODE, 0>(lo0, v_by[i]), kv_f16x2_by<CODE, 0>(lo1, v_by[i])};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 16) + kKeys * 2) = u32x2{kv_f16x2_by<CODE, 1>(lo0, v_by[i]), kv_f16x2_by<CODE, 1>(lo1, v_by[i])};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 32) + kKeys * 4) = u32x2{kv_f16x2_by<CODE, 0>(hi0, v_by[i]), kv_f16x2_by<CODE, 0>(hi1, v_by[i])};
+      *reinterpret_cast<u32x2 *>(lds + (to ^ 48) + kKeys * 6) = u32x2{kv_f16x2_by<CODE, 1>(hi0, v_by[i]), kv_f16x2_by<CODE, 1>(hi1, v_by[i])};
     }
   };
 
@@ -216,6 +235,16 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
   uint32_t at = 0;
   const uint32_t k_lane = k_at<D>(n32, hh), v_lane = kV + v_at(n32, hh);
   int n0 = n_lo;
+  // LDS operands that are read before the products of the ones before them: K's 32 keys and V's 32 channels at a time (277 -> 244 us for
+  // the prompts of 2 x 4096 tokens).  Channels of 64 have a third wave for that, which the registers would cost; fp32 and those of 256 have
+  // no registers left.
+  constexpr bool AHEAD = PARTS == 1 && D == 128;
+  f16x8 kf[2][AHEAD ? KS : 1];
+  auto read_k = [&](int x, uint32_t kl) {
+#pragma unroll
+    for (int k = 0; k < KS; k++) kf[x][AHEAD ? k : 0] = *reinterpret_cast<const f16x8 *>(lds + (kl ^ (32u * k)) + x * 32 * D * 2);
+    __builtin_amdgcn_sched_barrier(0);
+  };
   // one tile: its logits, weights and values.  SLOW: its V holds bare codes
   auto tile_of_keys = [&](auto is_slow, float f_v0, float f_v1, float tile_unit, float sk0, float sk1) {
     constexpr bool SLOW = decltype(is_slow)::value;
@@ -226,16 +255,23 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
     for (int x = 0; x < 2; x++) {
 #pragma unroll
       for (int e = 0; e < 16; e++) s[x][e] = 0.f;
+      if (AHEAD && x == 0) read_k(1, kl);
 #pragma unroll
       for (int k = 0; k < KS; k++) {
-        const f16x8 kf = *reinterpret_cast<const f16x8 *>(lds + (kl ^ (32u * k)) + x * 32 * D * 2);
+        const f16x8 kv = AHEAD ? kf[x][AHEAD ? k : 0] : *reinterpret_cast<const f16x8 *>(lds + (kl ^ (32u * k)) + x * 32 * D * 2);
 #pragma unroll
         for (int pt = PARTS - 1; pt >= 0; pt--) {
           const f16x8 qv = pt == 1 && !EARLY ? *reinterpret_cast<const f16x8 *>(q_lds + k * 1024) : qf[pt][k].v;
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qv, s[x], 0, 0, 0);
+          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kv, qv, s[x], 0, 0, 0);
         }
         if (!EARLY && k % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (not all operands at once)
       }
+    }
+    f16x8 vf[2][4];
+    if constexpr (AHEAD && !SLOW) {
+#pragma unroll
+      for (int k = 0; k < 4; k++) vf[0][k] = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)));
+      __builtin_amdgcn_sched_barrier(0);
     }
     const bool fresh = m == -INFINITY;
     const float ref = fresh ? 0.f : m;
@@ -292,13 +328,17 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (!SLOW) {
 #pragma unroll
-      for (int i = 0; i < MT; i++)
+      for (int i = 0; i < MT; i++) {
+        if (!AHEAD || i + 1 < MT) {
+          const int next_i = AHEAD ? i + 1 : i;
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-          const f16x8 vf = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)) + i * 32 * kKeys * 2);
-#pragma unroll
-          for (int pt = PARTS - 1; pt >= 0; pt--) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[pt][k].v, o[i], 0, 0, 0);
+          for (int k = 0; k < 4; k++) vf[next_i & 1][k] = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)) + next_i * 32 * kKeys * 2);
         }
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+          for (int pt = PARTS - 1; pt >= 0; pt--) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[i & 1][k], pf[pt][k].v, o[i], 0, 0, 0);
+      }
     } else {                                          // (a NaN block makes those rows NaN that see it)
       const float f0 = edge && n0 >= limit ? 0.f : f_v0, f1 = edge && n0 + 32 >= limit ? 0.f : f_v1;
 #pragma unroll
@@ -310,9 +350,9 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
           for (int e = 0; e < 16; e++) y[e] = 0.f;
 #pragma unroll
           for (int k = 2 * x; k < 2 * x + 2; k++) {
-            const f16x8 vf = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)) + i * 32 * kKeys * 2);
+            const f16x8 vk = *reinterpret_cast<const f16x8 *>(lds + (vl ^ (32u * k)) + i * 32 * kKeys * 2);
 #pragma unroll
-            for (int pt = PARTS - 1; pt >= 0; pt--) y = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[pt][k].v, y, 0, 0, 0);
+            for (int pt = PARTS - 1; pt >= 0; pt--) y = __builtin_amdgcn_mfma_f32_32x32x16_f16(vk, pf[pt][k].v, y, 0, 0, 0);
           }
 #pragma unroll
           for (int e = 0; e < 16; e++) o[i][e] = __builtin_fmaf(y[e], x ? f1 : f0, o[i][e]);
@@ -349,12 +389,14 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
     if constexpr (EARLY)
       while (n0 < n_wave && !slow) {
         const float u = next, k0 = staged_ks[0], k1 = staged_ks[1];
+        if constexpr (AHEAD) read_k(0, (uint32_t)opaque((int)(k_lane + at)));
         ahead();
         tile_of_keys(std::false_type{}, 0.f, 0.f, u, k0, k1);
         step();
       }
     while (n0 < n_wave && slow) {
       const float u = next, f0 = rel0, f1 = rel1, k0 = staged_ks[0], k1 = staged_ks[1];
+      if constexpr (AHEAD) read_k(0, (uint32_t)opaque((int)(k_lane + at)));
       ahead();
       tile_of_keys(std::true_type{}, f0, f1, u, k0, k1);
       step();
@@ -399,6 +441,27 @@ __global__ __launch_bounds__(WAVES * 64, D <= 128 ? 2 : 1) void kv_prompt_kernel
     if (a.lse2) a.lse2[row * R + r] = some ? z2 : INFINITY;
   }
 }
+
+// Workgroups that are through with an item draw the next one.  Dealt out by the hardware, which hands workgroups to the shader engines
+// in turn, whether or not another one has room, items of very different lengths (a padded batch, causal rows) kept a third of the CUs
+// waiting: 293 us for the prompts of 2 x 4096 tokens that take 262 us drawn (245 us with the operands' reads ahead).
+template <typename T, int CODE, int D, int DV, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D == 64 && sizeof(T) == 2 ? 3 : 2)
+void kv_prompt_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths, const int32_t *counts, T *out, float *lse, PromptArgs a) {
+  __shared__ int drawn;
+  int x = (int)blockIdx.x;
+  while (true) {
+    if (threadIdx.x == 0 && a.tickets) drawn = (int)gridDim.x + atomicAdd(a.tickets, 1);
+    kv_prompt_item<T, CODE, D, DV, WAVES>(c, d, q, lengths, counts, out, lse, a, x);
+    if (!a.tickets) return;
+    __syncthreads();
+    x = drawn;
+    if (x >= a.items) return;
+    __syncthreads();
+  }
+}
+
+__global__ void kv_no_tickets_kernel(int *tickets) { *tickets = 0; }
 
 // The splits' results together: D / 4 threads per row.  The workgroups behind those make the operands of the weights' second pass.
 template <typename T>
@@ -661,14 +724,17 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
 
 constexpr int waves_of(int D) { return D == 128 ? 8 : 4; }
 
+// Workgroups of the prompt kernel that a CU holds
+constexpr int per_cu(int D, int dtype) { return D == 64 ? dtype == NS_F32 ? 2 : 3 : 1; }
+
 int splits_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
   const int64_t rows = (int64_t)d.heads / c.heads_kv * d.tokens, per = waves_of(c.head_dim) * 32;
   const int64_t wgs = (rows + per - 1) / per * c.heads_kv * c.batch, cus = device_cu_count();
   // as many parts of the keys as fill the chip once, of 512 keys at least
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(c.head_dim == 64 ? 3 : 1) * cus / wgs, (int64_t)c.capacity / 512, 64}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({per_cu(c.head_dim, d.dtype) * cus / wgs, (int64_t)c.capacity / 512, 64}));
 }
 
-struct Layout { size_t o, ml, lse2, frags, factors, total; int splits; };
+struct Layout { size_t o, ml, lse2, frags, factors, tickets, total; int splits; };
 Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
   Layout w;
   w.splits = splits_of(c, d);
@@ -684,7 +750,8 @@ Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
   if (weights) off += kv_rows_frag_bytes(c, d);
   w.factors = off;
   if (weights) off += kv_rows_factor_bytes(c, d);
-  w.total = off;
+  w.tickets = off;
+  w.total = off + 256;
   return w;
 }
 
@@ -695,15 +762,24 @@ ns_status launch(const KvAttnArgs &a) {
   const Layout w = layout_of(c, a.d, a.w_out != nullptr);
   const int rows = a.d.heads / c.heads_kv * a.d.tokens, tiles = (rows + WAVES * 32 - 1) / (WAVES * 32);
   PromptArgs p{reinterpret_cast<float *>(a.ws + w.o), reinterpret_cast<float *>(a.ws + w.ml),
-               a.w_out ? reinterpret_cast<float *>(a.ws + w.lse2) : nullptr, w.splits};
+               a.w_out ? reinterpret_cast<float *>(a.ws + w.lse2) : nullptr, w.splits, 0, nullptr};
   // two tiles, or one and the second part of the queries
   const int tile_lds = kKeys * (D + DV) * 2, lds = DV == D ? 2 * tile_lds : tile_lds + WAVES * 32 * D * 2;
   const T *q = static_cast<const T *>(a.q);
   T *out = static_cast<T *>(a.out);
   ns_status st = reserve_lds_once(reinterpret_cast<const void *>(kv_prompt_kernel<T, CODE, D, DV, WAVES>), lds);
   if (st != NS_OK) return st;
-  const dim3 grid((unsigned)((int64_t)tiles * w.splits * (D / DV) * c.heads_kv * c.batch));
-  hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES>), grid, dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out, a.lse, p);
+  const int64_t items = (int64_t)tiles * w.splits * (D / DV) * c.heads_kv * c.batch;
+  if (items > 0x7fffffff - 65536) return fail(NS_ERR_UNSUPPORTED, "too many rows");
+  const int workgroups = (int)std::min<int64_t>(items, (int64_t)per_cu(D, a.d.dtype) * device_cu_count());
+  p.items = (int)items;                               // (with room for the numbers that are drawn in vain)
+  if (items > workgroups) {
+    p.tickets = reinterpret_cast<int *>(a.ws + w.tickets);
+    hipLaunchKernelGGL(kv_no_tickets_kernel, dim3(1), dim3(1), 0, a.stream, p.tickets);
+    if ((st = check_launch("kv_no_tickets_kernel")) != NS_OK) return st;
+  }
+  hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES>), dim3((unsigned)workgroups), dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out,
+                     a.lse, p);
   st = check_launch("kv_prompt_kernel");
   Frag *frags = reinterpret_cast<Frag *>(a.ws + w.frags);
   float *factors = reinterpret_cast<float *>(a.ws + w.factors);
