@@ -151,15 +151,16 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     // (the last tile of blocks of 32 may reach 32 keys beyond the capacity: their places take the 32 before once more.  Where a thread has
     // several pieces the first ones of all threads are before key 32, and whole pieces lie behind it)
     const uint32_t back = n0 + kKeys > c.capacity ? 32 * stride : 0u;
-    const uint32_t k_from = k_off - (KP == 1 && k_key >= 32 ? back : 0u), v_from = v_off - (VP == 1 && v_key >= 32 ? back : 0u);
+    const uint8_t *k_far = KP > 1 ? kp - back : kp, *v_far = VP > 1 ? vp - back : vp;
 #pragma unroll
     for (int i = 0; i < KP; i++)
-      kraw[i] = *reinterpret_cast<const u32x4 *>(kp + ((int64_t)i * KR * c.stride_t - (i * KR >= 32 ? back : 0u)) + k_from);
+      kraw[i] = *reinterpret_cast<const u32x4 *>((i * KR >= 32 ? k_far : kp) + (int64_t)i * KR * c.stride_t + (k_off - (KP == 1 && k_key >= 32 ? back : 0u)));
 #pragma unroll
     for (int i = 0; i < VP; i++)
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        vraw[i][j] = *reinterpret_cast<const uint32_t *>(vp + ((int64_t)(i * VR + j) * c.stride_t - (i * VR >= 32 ? back : 0u)) + v_from);
+        vraw[i][j] = *reinterpret_cast<const uint32_t *>((i * VR >= 32 ? v_far : vp) + (int64_t)(i * VR + j) * c.stride_t +
+                                                         (v_off - (VP == 1 && v_key >= 32 ? back : 0u)));
   };
   // V's scales: o is in units of `unit`, a tile's V in LDS in units of `next`, which is the same but where a much larger scale
   // comes along.  Where both halves' scales are next times a plain ratio, V is multiplied by that on its way (slow = false); else (a NaN, far
