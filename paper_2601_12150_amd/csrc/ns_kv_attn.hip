@@ -542,8 +542,15 @@ __global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, n
 int rows_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return d.heads / c.heads_kv * d.tokens; }
 
 // Row tiles of 16 that there are registers for
-constexpr int most_tiles(int head_dim, int dtype) { (void)dtype; return head_dim == 256 ? 1 : head_dim == 128 ? 2 : 4; }
-bool few_rows(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return rows_of(c, d) <= 16 * most_tiles(c.head_dim, d.dtype); }
+constexpr int most_tiles(int head_dim) { return head_dim == 256 ? 1 : head_dim == 128 ? 2 : 4; }
+// More rows are a prompt.  Of channels of 64 three and four tiles are bound by the products here, which prompts share out better: 45 us against 33
+// for 64 heads' 8192 tokens, 41 against 13 for 256 heads' 512.  Where there are few heads of many tokens this has more workgroups, by which its
+// finer shares win: 19 us against 37 for one head's 65536 tokens, 17 against 20 for 8 heads' 8192, 14 against 16 for 8 heads' 1024.
+bool few_rows(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
+  const int tiles = (rows_of(c, d) + 15) / 16;
+  if (tiles <= 2) return tiles <= most_tiles(c.head_dim);
+  return tiles <= most_tiles(c.head_dim) && c.capacity >= 1024 && (int64_t)c.batch * c.heads_kv * 16 < device_cu_count();
+}
 
 // Logits are 8 bytes a row and key, written and read; K read again D bytes a key.
 bool by_logits(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return 8 * rows_of(c, d) <= c.head_dim; }
@@ -608,7 +615,7 @@ ns_status launch_split(const KvAttnArgs &a) {
 
 template <typename T, int CODE, int D>
 ns_status launch_tiles(const KvAttnArgs &a) {
-  constexpr int most = most_tiles(D, sizeof(T) == 4 ? NS_F32 : NS_BF16);
+  constexpr int most = most_tiles(D);
   const int nt = (rows_of(a.c, a.d) + 15) / 16;
   if constexpr (most >= 4)
     if (nt > 2) return launch_split<T, CODE, D, 4>(a);

@@ -87,6 +87,42 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
   every = __builtin_amdgcn_readfirstlane(every);
   any = __builtin_amdgcn_readfirstlane(any);
 
+  // ---- codes on their way into LDS
+  const uint8_t *kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
+  const uint8_t *vb = static_cast<const uint8_t *>(c.v) + b * c.stride_b + h * c.stride_h + part * DV;
+  const float *ks = c.k_scale + row * (c.capacity / c.block), *vs = c.v_scale + row * (c.capacity / c.block);
+  const int lblock = 31 - __clz(c.block);
+  constexpr int KP = kKeys * D / 16 / THREADS, VP = kKeys / 4 * (DV / 4) / THREADS;      // pieces a thread has of K (16 codes) and V (4 x 4)
+  constexpr int KR = THREADS / (D / 16), VR = THREADS / (DV / 4) * 4;                    // keys between two of its pieces
+  static_assert((KP == 1 || (KR <= 32 && 32 % KR == 0)) && (VP == 1 || (VR <= 32 && 32 % VR == 0)), "key 32 begins a piece of all threads");
+  const int k_key = tid / (D / 16), v_key = tid / (DV / 4) * 4;
+  const uint32_t stride = (uint32_t)c.stride_t, k_off = (uint32_t)k_key * stride + tid % (D / 16) * 16, v_off = (uint32_t)v_key * stride + tid % (DV / 4) * 4;
+  u32x4 kraw[KP];
+  uint32_t vraw[VP][4];
+  float next_ks[2], next_vs[2], staged_ks[2] = {0.f, 0.f};    // scales of the fetched tile, and K's of the staged one
+  auto fetch = [&](int n0) {
+    const int n1 = min(n0 + 32, c.capacity - 32);   // (behind the capacity: masked, any scale will do)
+    next_ks[0] = ks[n0 >> lblock];
+    next_ks[1] = ks[n1 >> lblock];
+    next_vs[0] = vs[n0 >> lblock];
+    next_vs[1] = vs[n1 >> lblock];
+    const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
+    // (the last tile of blocks of 32 may reach 32 keys beyond the capacity: their places take the 32 before once more.  Where a thread has
+    // several pieces the first ones of all threads are before key 32, and whole pieces lie behind it)
+    const uint32_t back = n0 + kKeys > c.capacity ? 32 * stride : 0u;
+    const uint8_t *k_far = KP > 1 ? kp - back : kp, *v_far = VP > 1 ? vp - back : vp;
+#pragma unroll
+    for (int i = 0; i < KP; i++)
+      kraw[i] = *reinterpret_cast<const u32x4 *>((i * KR >= 32 ? k_far : kp) + (int64_t)i * KR * c.stride_t + (k_off - (KP == 1 && k_key >= 32 ? back : 0u)));
+#pragma unroll
+    for (int i = 0; i < VP; i++)
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        vraw[i][j] = *reinterpret_cast<const uint32_t *>((i * VR >= 32 ? v_far : vp) + (int64_t)(i * VR + j) * c.stride_t +
+                                                         (v_off - (VP == 1 && v_key >= 32 ? back : 0u)));
+  };
+  if (n_lo < n_hi) fetch(n_lo);
+
   // ---- queries
   Frag qf[PARTS][KS];
   float factor;
@@ -128,40 +164,6 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     for (int s = 0; s < KS; s++) *reinterpret_cast<f16x8 *>(q_lds + s * 1024) = qf[PARTS - 1][s].v;
   }
 
-  // ---- codes on their way into LDS
-  const uint8_t *kb = static_cast<const uint8_t *>(c.k) + b * c.stride_b + h * c.stride_h;
-  const uint8_t *vb = static_cast<const uint8_t *>(c.v) + b * c.stride_b + h * c.stride_h + part * DV;
-  const float *ks = c.k_scale + row * (c.capacity / c.block), *vs = c.v_scale + row * (c.capacity / c.block);
-  const int lblock = 31 - __clz(c.block);
-  constexpr int KP = kKeys * D / 16 / THREADS, VP = kKeys / 4 * (DV / 4) / THREADS;      // pieces a thread has of K (16 codes) and V (4 x 4)
-  constexpr int KR = THREADS / (D / 16), VR = THREADS / (DV / 4) * 4;                    // keys between two of its pieces
-  static_assert((KP == 1 || (KR <= 32 && 32 % KR == 0)) && (VP == 1 || (VR <= 32 && 32 % VR == 0)), "key 32 begins a piece of all threads");
-  const int k_key = tid / (D / 16), v_key = tid / (DV / 4) * 4;
-  const uint32_t stride = (uint32_t)c.stride_t, k_off = (uint32_t)k_key * stride + tid % (D / 16) * 16, v_off = (uint32_t)v_key * stride + tid % (DV / 4) * 4;
-  u32x4 kraw[KP];
-  uint32_t vraw[VP][4];
-  float next_ks[2], next_vs[2], staged_ks[2] = {0.f, 0.f};    // scales of the fetched tile, and K's of the staged one
-  auto fetch = [&](int n0) {
-    const int n1 = min(n0 + 32, c.capacity - 32);   // (behind the capacity: masked, any scale will do)
-    next_ks[0] = ks[n0 >> lblock];
-    next_ks[1] = ks[n1 >> lblock];
-    next_vs[0] = vs[n0 >> lblock];
-    next_vs[1] = vs[n1 >> lblock];
-    const uint8_t *kp = kb + (int64_t)n0 * c.stride_t, *vp = vb + (int64_t)n0 * c.stride_t;
-    // (the last tile of blocks of 32 may reach 32 keys beyond the capacity: their places take the 32 before once more.  Where a thread has
-    // several pieces the first ones of all threads are before key 32, and whole pieces lie behind it)
-    const uint32_t back = n0 + kKeys > c.capacity ? 32 * stride : 0u;
-    const uint8_t *k_far = KP > 1 ? kp - back : kp, *v_far = VP > 1 ? vp - back : vp;
-#pragma unroll
-    for (int i = 0; i < KP; i++)
-      kraw[i] = *reinterpret_cast<const u32x4 *>((i * KR >= 32 ? k_far : kp) + (int64_t)i * KR * c.stride_t + (k_off - (KP == 1 && k_key >= 32 ? back : 0u)));
-#pragma unroll
-    for (int i = 0; i < VP; i++)
-#pragma unroll
-      for (int j = 0; j < 4; j++)
-        vraw[i][j] = *reinterpret_cast<const uint32_t *>((i * VR >= 32 ? v_far : vp) + (int64_t)(i * VR + j) * c.stride_t +
-                                                         (v_off - (VP == 1 && v_key >= 32 ? back : 0u)));
-  };
   // V's scales: o is in units of `unit`, a tile's V in LDS in units of `next`, which is the same but where a much larger scale
   // comes along.  Where both halves' scales are next times a plain ratio, V is multiplied by that on its way (slow = false); else (a NaN, far
   // smaller ones, the caller's own that are no powers of two) LDS has the bare codes, and the products are multiplied.
@@ -240,6 +242,10 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
   // the prompts of 2 x 4096 tokens).  Channels of 64 have a third wave for that, which the registers would cost; fp32 and those of 256 have
   // no registers left.
   constexpr bool AHEAD = PARTS == 1 && D == 128;
+  // The two waves of a SIMD: one stages the next tile before its own products, the other between them and the values', so that one has
+  // matrix instructions for most of what the other has of others (243 -> 239 us; 316 -> 295 us for 512 queries behind 32768 tokens;
+  // fp32, whose products are twice as many: 463 against 476 us without and with it)
+  constexpr bool LATE = PARTS == 1 && WAVES == 8;
   f16x8 kf[2][AHEAD ? KS : 1];
   auto read_k = [&](int x, uint32_t kl) {
 #pragma unroll
@@ -247,7 +253,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     __builtin_amdgcn_sched_barrier(0);
   };
   // one tile: its logits, weights and values.  SLOW: its V holds bare codes
-  auto tile_of_keys = [&](auto is_slow, float f_v0, float f_v1, float tile_unit, float sk0, float sk1) {
+  auto tile_of_keys = [&](auto is_slow, auto between, float f_v0, float f_v1, float tile_unit, float sk0, float sk1) {
     constexpr bool SLOW = decltype(is_slow)::value;
     const bool edge = n0 + kKeys > every;
     const uint32_t kl = (uint32_t)opaque((int)(k_lane + at)), vl = (uint32_t)opaque((int)(v_lane + at));
@@ -327,6 +333,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
         }
       }
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+    between();
     if constexpr (!SLOW) {
 #pragma unroll
       for (int i = 0; i < MT; i++) {
@@ -378,12 +385,12 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     }
   };
   if (n_lo < n_hi) {
-    fetch(n_lo);
     stage(n_lo, 0);
     unit = next;
     if (EARLY && n_lo + kKeys < n_hi) fetch(n_lo + kKeys);
     __syncthreads();
   }
+  const bool late = LATE && wave >= 4;
   // (loops of their own for the two kinds of tiles, and for those that the wave has no part in: o stays in its registers)
   const int n_wave = min(n_hi, any);
   while (n0 < n_wave) {
@@ -391,15 +398,15 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
       while (n0 < n_wave && !slow) {
         const float u = next, k0 = staged_ks[0], k1 = staged_ks[1];
         if constexpr (AHEAD) read_k(0, (uint32_t)opaque((int)(k_lane + at)));
-        ahead();
-        tile_of_keys(std::false_type{}, 0.f, 0.f, u, k0, k1);
+        if (!late) ahead();
+        tile_of_keys(std::false_type{}, [&] { if (late) ahead(); }, 0.f, 0.f, u, k0, k1);
         step();
       }
     while (n0 < n_wave && slow) {
       const float u = next, f0 = rel0, f1 = rel1, k0 = staged_ks[0], k1 = staged_ks[1];
       if constexpr (AHEAD) read_k(0, (uint32_t)opaque((int)(k_lane + at)));
       ahead();
-      tile_of_keys(std::true_type{}, f0, f1, u, k0, k1);
+      tile_of_keys(std::true_type{}, [] {}, f0, f1, u, k0, k1);
       step();
     }
   }

@@ -331,6 +331,9 @@ def test_attention_of_blocks_of_different_sizes(nb, code, dtype, D, G, T, kind):
 @pytest.mark.parametrize("dtype,code,B,H,G,D,block,N,T,padded", [
     ("bf16", "i8", 150, 2, 8, 64, 64, 2048, 3, False),             # 24 rows of many sequences: shares of the keys that cross them
     ("bf16", "e4m3", 129, 2, 1, 128, 128, 4096, 1, False),         # a workgroup per sequence and head
+    ("bf16", "e4m3", 2, 2, 8, 64, 64, 2048, 8, True),              # 64 rows of few heads, and of more
+    ("f32", "i8", 3, 1, 4, 64, 32, 1056, 12, True),
+    ("bf16", "i8", 9, 2, 8, 64, 64, 2048, 8, True),
     ("f32", "i8", 40, 8, 2, 64, 32, 320, 150, True),               # more tiles of rows than the chip takes at once
     ("bf16", "i8", 48, 8, 2, 64, 32, 320, 150, True),
     ("bf16", "e4m3", 40, 8, 2, 128, 64, 320, 150, True),
@@ -341,7 +344,7 @@ def test_attention_of_blocks_of_different_sizes(nb, code, dtype, D, G, T, kind):
 def test_attention_of_many_sequences(nb, dtype, code, B, H, G, D, block, N, T, padded):
     rng = np.random.default_rng(B)
     lengths = [int(n) for n in rng.integers(0, N + 1, B)]
-    lengths[:4] = [N, 0, 1, T]
+    lengths[:4] = [N, 0, 1, T][:B]
     counts = [int(n) for n in rng.integers(0, T + 1, B)] if padded else None
     attention_case(nb, dtype, code, B, H, G, D, block, N, T, lengths, counts)
 
