@@ -535,15 +535,17 @@ __global__ __launch_bounds__(256) void kv_weights_rows_kernel(ns_kv_cache c, ns_
   if (tile < (R + 15) / 16) kv_rows_tile(c, d, q, blockIdx.z, blockIdx.y, tile, threadIdx.x & 63, frags, factors);
 }
 
-// Many rows: a wave's keys stay, the rows' operands come from the L2, an operand serves KX tiles of 16 keys.
-template <int PARTS, int CODE, int D, int KX>
+// Many rows: a wave's keys stay, the rows' operands come from the L2, an operand serves KX tiles of 16 keys.  SHARE: a workgroup's
+// waves have the same keys and take the tiles of rows in turn.
+template <int PARTS, int CODE, int D, int KX, bool SHARE>
 __global__ __launch_bounds__(256, 2) void kv_weights_sum_kernel(ns_kv_cache c, ns_kv_attn_desc d, const int32_t *lengths, const int32_t *counts,
                                                              const Frag *frags, const float *factors, const float *lse2, const float *w_in,
                                                              float *w_out) {
   constexpr int KS = D / 32, kKeysOf = 16 * KX;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = d.heads / c.heads_kv, R = G * d.tokens, tiles = (R + 15) / 16, lblock = 31 - __clz(c.block);
-  const int h = blockIdx.y, b = blockIdx.z, n0 = ((int)blockIdx.x * 4 + wave) * kKeysOf;
+  const int h = blockIdx.y, b = blockIdx.z, n0 = (SHARE ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave) * kKeysOf;
+  constexpr int STEP = SHARE ? 4 : 1;
   __shared__ float sums[4][kKeysOf][17];
   const int length = kv_length(lengths, b, c.capacity), count = kv_count(counts, b, d.tokens);
   const int64_t row = (int64_t)b * c.heads_kv + h;
@@ -578,7 +580,8 @@ __global__ __launch_bounds__(256, 2) void kv_weights_sum_kernel(ns_kv_cache c, n
       fr = factors[row * tiles * 16 + r];
       ref = lse2[row * R + min(r, R - 1)];            // (rows that are none are masked)
     };
-    load_rows(first);
+    const int from_tile = first + (SHARE ? wave : 0);
+    load_rows(min(from_tile, last - 1));
     Frag kf[KX][KS];
 #pragma unroll
     for (int x = 0; x < KX; x++)
@@ -587,7 +590,7 @@ __global__ __launch_bounds__(256, 2) void kv_weights_sum_kernel(ns_kv_cache c, n
     f32x4 acc[KX];
 #pragma unroll
     for (int x = 0; x < KX; x++) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int tile = first; tile < last; tile++) {
+    for (int tile = from_tile; tile < last; tile += STEP) {
       const int r = tile * 16 + n16;
       const float f_row = fr, z0 = ref;
       f32x4 s[KX];
@@ -597,7 +600,7 @@ __global__ __launch_bounds__(256, 2) void kv_weights_sum_kernel(ns_kv_cache c, n
       for (int k = PARTS * KS - 1; k >= 0; k--)       // (the smaller parts first)
 #pragma unroll
         for (int x = 0; x < KX; x++) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x][k % KS].v, next[k].v, s[x], 0, 0, 0);
-      if (tile + 1 < last) load_rows(tile + 1);
+      if (tile + STEP < last) load_rows(tile + STEP);
 #pragma unroll
       for (int x = 0; x < KX; x++) {
         const float f = f_row * sk[x];
@@ -621,15 +624,20 @@ __global__ __launch_bounds__(256, 2) void kv_weights_sum_kernel(ns_kv_cache c, n
     for (int x = 0; x < KX; x++)
 #pragma unroll
       for (int e = 0; e < 4; e++) to[16 * x + 4 * g + e][n16] = acc[x][e];
-    __builtin_amdgcn_wave_barrier();                  // (a wave's LDS operations are in order)
+    if (SHARE)
+      __syncthreads();
+    else
+      __builtin_amdgcn_wave_barrier();                // (a wave's LDS operations are in order)
     const int from = lane % kKeysOf;
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; i++) part[i % 4] += to[from][i];
+    for (int w = 0; w < STEP; w++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) part[i % 4] += (SHARE ? sums[w] : to)[from][i];
     sum = (part[0] + part[1]) + (part[2] + part[3]);
   }
   const int n = n0 + lane;
-  if (lane >= kKeysOf || n >= c.capacity || (n >= length && w_in == w_out)) return;
+  if ((SHARE && wave > 0) || lane >= kKeysOf || n >= c.capacity || (n >= length && w_in == w_out)) return;
   const int64_t at = row * c.capacity + n;
   w_out[at] = (w_in ? w_in[at] : 0.f) + sum;
 }
@@ -826,14 +834,20 @@ ns_status weights_sum(const KvAttnArgs &a, const Frag *frags, const float *facto
     }
     return go(kv_weights_stream_kernel<PARTS, CODE, 128, 2>);
   }
-  const int keys = PARTS * a.c.head_dim == 512 ? 128 : 256;            // of a workgroup
+  // a wave has the operands of 64 keys, or 32, in registers.  Its workgroup the same ones, with the rows shared out, where there are fewer
+  // than CUs of workgroups with keys of their own (16 heads of 64, 576 rows and keys, all of the call: 35 -> 27 us; 2048 rows, 320 keys: 65 -> 36)
+  constexpr int KX256 = PARTS == 2 ? 2 : 4;
+  const int most = a.c.head_dim == 256 ? 64 * KX256 : 256;
+  const bool share = (int64_t)((a.c.capacity + most - 1) / most) * a.c.heads_kv * a.c.batch < device_cu_count();
+  const int keys = share ? most / 4 : most;
   const dim3 grid((unsigned)((a.c.capacity + keys - 1) / keys), (unsigned)a.c.heads_kv, (unsigned)a.c.batch);
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, a.c, a.d, a.lengths, a.counts, frags, factors, lse2, a.w_in, a.w_out);
+  auto go = [&](auto kernel, auto shared) {
+    hipLaunchKernelGGL(share ? shared : kernel, grid, dim3(256), 0, a.stream, a.c, a.d, a.lengths, a.counts, frags, factors, lse2, a.w_in, a.w_out);
     return check_launch("kv_weights_sum_kernel");
   };
-  return a.c.head_dim == 64 ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 4>) : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 4>)
-                                                                                                 : go(kv_weights_sum_kernel<PARTS, CODE, 256, PARTS == 2 ? 2 : 4>);
+  return a.c.head_dim == 64    ? go(kv_weights_sum_kernel<PARTS, CODE, 64, 4, false>, kv_weights_sum_kernel<PARTS, CODE, 64, 4, true>)
+         : a.c.head_dim == 128 ? go(kv_weights_sum_kernel<PARTS, CODE, 128, 4, false>, kv_weights_sum_kernel<PARTS, CODE, 128, 4, true>)
+                               : go(kv_weights_sum_kernel<PARTS, CODE, 256, KX256, false>, kv_weights_sum_kernel<PARTS, CODE, 256, KX256, true>);
 }
 
 }  // namespace
