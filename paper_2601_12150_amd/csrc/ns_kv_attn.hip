@@ -552,10 +552,16 @@ bool few_rows(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
   return tiles <= most_tiles(c.head_dim) && c.capacity >= 1024 && (int64_t)c.batch * c.heads_kv * 16 < device_cu_count();
 }
 
-// Logits are 8 bytes a row and key, written and read; K read again D bytes a key.
-bool by_logits(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return 8 * rows_of(c, d) <= c.head_dim; }
+// Weights: logits are 8 bytes a row and key, written and read; K read again is D bytes a key, its products and a launch.  32 heads' 16384
+// tokens, logits against K again: 8 rows of 64 channels 26.5 us against 28.5, 16 rows 35.9 against 29.2; of 128 channels 36.6 against 44.8 and
+// 46.1 against 45.7 (8 heads' 131072: 4 rows 56 against 76, 16 rows 87 against 77); 16 rows of 256 channels 77 against 82.
+bool by_logits(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return rows_of(c, d) <= (c.head_dim == 256 ? 16 : 10); }
+// A workgroup per sequence and head, which spares the records and their join: where a head's tokens are few (8 heads' 1024 of 64 channels 7.5 us
+// against 9.1 shared out, 2048: 11.1 against 9.2; 512 of 128 channels 8.2 against 9.8, 1024: 11.0 against 9.8), and where there is one
+// for every CU (256 heads' 4096 of 128 channels 43.5 against 49.8; of more tokens, still 98.5 against 104.9 for 8192, a single long sequence
+// among short ones would have its heads' workgroups run alone for too long).
 bool alone(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
-  return rows_of(c, d) <= 16 && c.capacity <= ((int64_t)c.batch * c.heads_kv >= device_cu_count() ? 4096 : 1024);
+  return rows_of(c, d) <= 16 && ((int64_t)c.capacity * c.head_dim <= 65536 || (c.capacity <= 4096 && (int64_t)c.batch * c.heads_kv >= device_cu_count()));
 }
 
 struct Layout { size_t o, ml, lse2, logits, frags, factors, total; int workgroups; };

@@ -4,7 +4,7 @@
 // The tokens that stay are found by the key (an order-preserving integer image of the weight) of the last of them: digits of 11,
 // 11 and 10 bits, each from a histogram of the keys that share the digits before it (radix select).  Then all tokens with a larger
 // key stay, and of those with this very key the first ones.
-//   kv_select_kernel: caches of up to 32768 tokens; one workgroup per sequence and head has all keys in registers, one launch.
+//   kv_select_kernel: caches of up to 16384 tokens; one workgroup per sequence and head has all keys in registers, one launch.
 //   kv_digit_kernel, kv_place_kernel: longer ones, a workgroup per 8192 tokens; a launch for every digit and one that places.
 //   kv_move_kernel: a workgroup per block of the new cache; its codes are read once and stay in registers until the scale is known.
 #include "ns_kv.h"
@@ -15,7 +15,9 @@ namespace {
 
 constexpr int kSelect = 1024, kWaves = kSelect / 64;
 constexpr int kBits[3] = {11, 11, 10}, kShift[3] = {21, 10, 0}, kBins = 2048;
-constexpr int kHeld = 32768;                      // tokens that one workgroup selects from
+// Tokens that one workgroup selects from: 8 heads' 16384 to 1000 take 21 us with, 31 without (the move included); one of 32768 would take
+// 34 against 32.
+constexpr int kHeld = 16384;
 constexpr int kChunkKeys = 8, kChunk = kSelect * kChunkKeys;
 
 // larger weight <=> larger key; -0 and +0 alike, NaN above everything
@@ -375,7 +377,7 @@ ns_status launch_kv_evict(const ns_kv_cache &from, const ns_kv_cache &to, const 
   if (from.capacity <= kHeld) {
     const dim3 grid((unsigned)from.heads_kv, (unsigned)from.batch);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSelect), 0, s, a); };
-    from.capacity <= 2 * kSelect ? go(kv_select_kernel<2>) : from.capacity <= 8 * kSelect ? go(kv_select_kernel<8>) : from.capacity <= 16 * kSelect ? go(kv_select_kernel<16>) : go(kv_select_kernel<32>);
+    from.capacity <= 2 * kSelect ? go(kv_select_kernel<2>) : from.capacity <= 8 * kSelect ? go(kv_select_kernel<8>) : go(kv_select_kernel<16>);
     st = check_launch("kv_select_kernel");
   } else {
     const dim3 grid((unsigned)chunks_of(from.capacity), (unsigned)from.heads_kv, (unsigned)from.batch);
