@@ -135,6 +135,8 @@ __device__ __forceinline__ void weigh(const ns_kv_cache &c, const ns_kv_attn_des
 constexpr int per_cu(bool f32, int D, int NT) { return NT * D <= 128 || (!f32 && D == 128 && NT == 2) ? 2 : 1; }
 
 // T: float takes its queries, and the weights, as the sum of two fp16 numbers.  ALONE: a workgroup has a head to itself.
+// Measured, bf16, 128 channels, 4 rows a head: 131001 tokens of 8 heads 46 us (268 MB and 17 MB of logits, 6.2 TB/s); a workgroup for each of
+// 8 heads of 32 sequences of 63708 tokens together 33 us (131 MB, 3.9 TB/s; the longest one sets it).  32 rows: 58990 tokens of 8 heads 32 us (121 MB, 3.7).
 template <typename T, int CODE, int D, int NT, int WAVES, bool ALONE>
 __global__ __launch_bounds__(WAVES * 64, ALONE ? (D == 256 ? 1 : 2) : per_cu(sizeof(T) == 4, D, NT))
 void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths, const int32_t *counts, T *out, float *lse, SplitArgs a) {
@@ -446,7 +448,7 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
 }
 
 // The first R workgroups of a head: a row's joined result each.  The others: the weights of 1024 positions each from the rows'
-// logits, or the operands for the weights' second pass.
+// logits, or the operands for the weights' second pass.  Bound by latency: 8 to 10 us.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv_attn_join_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths,
                                                                 const int32_t *counts, T *out, float *lse, SplitArgs a) {

@@ -23,7 +23,8 @@ template <> struct Row8<bf16_t> {
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // One workgroup per block of tokens that a sequence's new tokens may touch, head, and keys or values.  The scale needs the
-// largest magnitude of all new values of the block: a thread has its up to PIECES times 8 in registers until it is known.
+// largest magnitude of all new values of the block: a thread has its up to PIECES times 8 in registers until it is known, so that they are
+// read once.  Bound by the reads and writes: 8404 tokens of 8 heads of 128 channels in bf16, 52 MB, 16 us (3.2 TB/s); one token 3.5 us.
 template <typename T, int CODE, int PIECES>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int tokens, const T *k, const T *v, int64_t sb, int64_t sh,
                                                              int64_t st, const int32_t *start, const int32_t *counts) {
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int 
   if (tid == 0) *scale = s;
 }
 
-// 16 codes per thread.
+// 16 codes per thread.  Bound by the writes: 16384 positions of 8 heads of 128 channels in bf16, 84 MB, 15 us (5.5 TB/s).
 template <typename T, int CODE>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(ns_kv_cache c, const int32_t *lengths, int first, int tokens, T *k_out, T *v_out) {
   const int b = blockIdx.z, h = blockIdx.y >> 1, value = blockIdx.y & 1;

