@@ -524,7 +524,10 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 8, [&]() -> PyObject * {
     const Cache c = read_cache(a[0]);
     const at::Tensor &lengths = tensor(a[1], "lengths");
-    const int32_t first = int32(a[2], "first"), tokens = a[3] == Py_None ? c.c.capacity - first : int32(a[3], "tokens");
+    const int32_t first = int32(a[2], "first");
+    if (first < 0 || first >= c.c.capacity) value_error("first must lie within the capacity");
+    const int32_t tokens = a[3] == Py_None ? c.c.capacity - first : int32(a[3], "tokens");
+    if (tokens < 1 || tokens > c.c.capacity - first) value_error("tokens must be positive and end within the capacity");
     const int bf = PyObject_IsTrue(a[4]);
     if (bf < 0) throw PyFail{};
     const auto dt = bf ? at::kBFloat16 : at::kFloat;
@@ -532,7 +535,7 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
     at::Tensor out[2] = {optional(a[5], "k_out"), optional(a[6], "v_out")};
     for (at::Tensor &t : out) {
       if (!t.defined()) {
-        t = empty({c.c.batch, c.c.heads_kv, tokens > 0 ? tokens : 0, c.c.head_dim}, dt, c.k);
+        t = empty({c.c.batch, c.c.heads_kv, tokens, c.c.head_dim}, dt, c.k);
       } else if (t.scalar_type() != dt || !t.is_contiguous() || t.sizes() != at::IntArrayRef({c.c.batch, c.c.heads_kv, tokens, c.c.head_dim})) {
         value_error("k_out and v_out must be contiguous [B,H,tokens,D] tensors of the asked dtype");
       }
@@ -588,8 +591,9 @@ PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int32_t keep = int32(a[4], "keep"), G = int32(a[5], "n_global"), recent = int32(a[6], "n_recent");
     const float *wp = weights_of(w, c.c.batch, c.c.heads_kv, c.c.capacity, "weights");
     const int32_t *lp = counts_of(lengths, c, "lengths");
+    if (keep < 1 || keep > c.c.capacity) value_error("keep must be in [1, capacity]");
     const int64_t B = c.c.batch, H = c.c.heads_kv;
-    const at::Tensor kept = empty({B, H, keep > 0 ? keep : 0}, at::kInt, c.k), left = empty({B}, at::kInt, c.k);
+    const at::Tensor kept = empty({B, H, keep}, at::kInt, c.k), left = empty({B}, at::kInt, c.k);
     const at::Tensor w_out = empty({B, H, to.c.capacity}, at::kFloat, c.k);
     const at::Tensor ws = workspace(a[7], kv_cache_evict_workspace_bytes(&c.c, keep), c.k);
     on_current_device({&c.k, &c.v, &c.k_scale, &c.v_scale, &to.k, &to.v, &to.k_scale, &to.v_scale, &w, &lengths, &ws});

@@ -154,7 +154,7 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
     const int share = tiles_all.share(gridDim.x), total = tiles_all.all();
     if ((int)blockIdx.x > (total - 1) / share || total == 0) return;
     u = share * (int)blockIdx.x;
-    u_end = min(u + share, total);
+    u_end = total - u < share ? total : u + share;
   }
 
   // ---- the piece of a head's tokens in hand, and codes on their way

@@ -334,6 +334,11 @@ def test_attention_of_blocks_of_different_sizes(nb, code, dtype, D, G, T, kind):
     ("bf16", "e4m3", 2, 2, 8, 64, 64, 2048, 8, True),              # 64 rows of few heads, and of more
     ("f32", "i8", 3, 1, 4, 64, 32, 1056, 12, True),
     ("bf16", "i8", 9, 2, 8, 64, 64, 2048, 8, True),
+    ("bf16", "i8", 2, 2, 4, 256, 64, 1280, 4, True),               # 16, 15 and 10 rows: weights from logits or from K again
+    ("f32", "e4m3", 3, 2, 3, 128, 32, 1600, 5, True),
+    ("bf16", "e4m3", 2, 3, 5, 64, 128, 2048, 2, False),
+    ("f32", "i8", 2, 2, 4, 64, 64, 512, 4, True),                  # the same, a workgroup per head
+    ("bf16", "i8", 3, 2, 4, 256, 32, 256, 4, False),
     ("f32", "i8", 40, 8, 2, 64, 32, 320, 150, True),               # more tiles of rows than the chip takes at once
     ("bf16", "i8", 48, 8, 2, 64, 32, 320, 150, True),
     ("bf16", "e4m3", 40, 8, 2, 128, 64, 320, 150, True),

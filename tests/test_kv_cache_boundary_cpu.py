@@ -165,6 +165,13 @@ def test_the_binding_checks_its_tensors(nb):
     with pytest.raises(ValueError):
         nb.kv_cache_read(cache, n, k_out=torch.zeros((B, H, 3, D)))
     # all in order, but not on a GPU
+    # before anything of such a size is allocated
+    for args in ((-2 ** 31,), (-1, 5), (N,), (0, 2 ** 31 - 1), (0, 0), (5, N - 4)):
+        with pytest.raises(ValueError, match="capacity"):
+            nb.kv_cache_read(cache, n, *args)
+    for keep in (0, -1, N + 1, 2 ** 31 - 1):
+        with pytest.raises(ValueError, match="keep"):
+            nb.kv_cache_evict(cache, to, w, n, keep)
     for f in (lambda: nb.kv_cache_append(cache, x, x, n), lambda: nb.kv_cache_read(cache, n), lambda: nb.kv_cache_attn(cache, q, n, want_weights=True),
               lambda: nb.kv_cache_evict(cache, to, w, n, 10)):
         with pytest.raises(ValueError, match="GPU"):
