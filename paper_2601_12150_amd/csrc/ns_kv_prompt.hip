@@ -10,7 +10,7 @@
 // Rows are numbered r = token * group + head, so that a causal row tile ends after few more keys than it begins with.
 //
 // Measured: two sequences' 6627 prompt tokens, 32 query heads of 128 channels on 8, bf16 and int8: 240 us, 790 TFLOP/s (512 queries behind
-// 32768 tokens 930; fp32 590); 512 queries of 16 heads of 64 channels across 16385 tokens 61 us, 280 TFLOP/s.  A tile of 64 keys
+// 32768 tokens 890 to 930; fp32 590); 512 queries of 16 heads of 64 channels across 16385 tokens 61 us, 280 TFLOP/s.  A tile of 64 keys
 // by 32 rows of 128 channels is 1024 cycles of products, 512 of exponentials, about 1000 of other vector instructions and 256 of LDS reads of
 // the CU's 2048 for its eight waves: no one of them alone is the bound.
 #include "ns_kv.h"
@@ -746,6 +746,9 @@ __global__ __launch_bounds__(256, 2) void kv_weights_stream_kernel(ns_kv_cache c
 
 // ---- host side
 
+// Waves of a workgroup: a tile's conversion serves the rows of all of them.  128 channels, 8 waves against two workgroups of 4: 245 us against
+// 270 for the prompts of 2 x 4096 tokens, fp32 530 against 565.  64 channels have three workgroups of 4 instead (a tile is 16 codes for each
+// thread of 4 waves), 256 channels registers for one wave a SIMD.
 constexpr int waves_of(int D) { return D == 128 ? 8 : 4; }
 
 // Workgroups of the prompt kernel that a CU holds
