@@ -340,7 +340,8 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
           top = half_swap_max(row_swap_max(top));
           const bool moved = top > kRoom || (fresh && top > -INFINITY);
           const float move = moved ? top - kLift : 0.f;
-          const float fade = __builtin_amdgcn_exp2f(-move);
+          // (a fresh row's sums are 0, or NaN: not times a factor beyond fp32 where its logits are far below 0)
+          const float fade = __builtin_amdgcn_exp2f(fminf(-move, 0.f));
 #pragma unroll
           for (int i = 0; i < 8; i++) z[i] -= move;
           if (moved) m[nt] = ref + move;

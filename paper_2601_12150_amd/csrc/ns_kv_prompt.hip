@@ -309,7 +309,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
       top = half_swap_max(top);
       const bool moved = top > kRoom || (fresh && top > -INFINITY);
       const float move = moved ? top - kLift : 0.f;
-      float fade = __builtin_amdgcn_exp2f(-move);
+      float fade = __builtin_amdgcn_exp2f(fminf(-move, 0.f));      // (a fresh row's sums are 0, or NaN: not times a factor beyond fp32)
 #pragma unroll
       for (int x = 0; x < 2; x++)
 #pragma unroll
