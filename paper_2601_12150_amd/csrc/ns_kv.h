@@ -36,6 +36,9 @@ __device__ __forceinline__ int kv_count(const int32_t *counts, int b, int tokens
   return counts ? min(max(counts[b], 0), tokens) : tokens;
 }
 
+// Tiles per workgroup where `tiles` of them (up to 2^31 - 1) are shared out
+__host__ __device__ constexpr int kv_share(int tiles, int workgroups) { return tiles ? (tiles - 1) / workgroups + 1 : 1; }
+
 // ---- codes.  CODE: ns_kv_code
 // the four values of a dword of codes (int8: bytes c + 128 have a conversion of their own)
 template <int CODE>

@@ -65,7 +65,7 @@ struct Tiles {
     return sum * heads_kv;
   }
   // tiles per workgroup
-  __device__ __forceinline__ int share(int workgroups) const { return max((all() + workgroups - 1) / workgroups, 1); }
+  __device__ __forceinline__ int share(int workgroups) const { return kv_share(all(), workgroups); }
   // the tiles of the sequences before b
   __device__ __forceinline__ int before(int b) const {
     if (b == 0) return 0;

@@ -1,0 +1,28 @@
+"""The 8-bit key/value cache at the limits of what its entry points take, without a GPU."""
+import os
+import subprocess
+
+import pytest
+
+from paper_2601_12150_amd import build as hip_build
+
+
+@pytest.mark.skipif(not os.path.exists(hip_build.HIPCC), reason="needs hipcc")
+def test_shares_of_as_many_tiles_as_there_may_be(tmp_path):
+    """Every workgroup's share of the tiles covers them all, without one that is not needed, up to the last number that is let through."""
+    src = tmp_path / "shares.hip"
+    src.write_text('#include "%s"\n' % os.path.join(hip_build.CSRC, "ns_kv.h") + """
+constexpr bool good(int tiles, int workgroups) {
+  const long long share = ns::kv_share(tiles, workgroups);
+  return share >= 1 && share * workgroups >= tiles && (tiles == 0 || (share - 1) * workgroups < tiles);
+}
+constexpr bool all_good() {
+  for (int workgroups : {1, 255, 256, 512, 1024})
+    for (int tiles : {0, 1, 511, 512, 513, 1 << 30, 0x7fffffff - 511, 0x7fffffff - 1, 0x7fffffff})
+      if (!good(tiles, workgroups)) return false;
+  return true;
+}
+static_assert(all_good(), "shares");
+""")
+    r = subprocess.run([hip_build.HIPCC, "--offload-host-only", "-fsyntax-only", "-std=c++17", str(src)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout[-2000:]
