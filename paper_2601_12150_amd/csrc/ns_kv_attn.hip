@@ -164,8 +164,8 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
   const float *ks = nullptr, *vs = nullptr;
   auto piece_at = [&](int tile) {
     if constexpr (ALONE) {
-      b = (int)blockIdx.x / c.heads_kv;
-      h = (int)blockIdx.x - b * c.heads_kv;
+      b = (int)blockIdx.y;
+      h = (int)blockIdx.x;
       length = kv_length(lengths, b, c.capacity);
       n_hi = length;
     } else {
@@ -604,7 +604,7 @@ ns_status launch_split(const KvAttnArgs &a) {
   if constexpr (NT == 1)
     if (alone(c, a.d)) {
       constexpr int WAVES = D == 256 ? 4 : 8;       // (LDS)
-      hipLaunchKernelGGL((kv_attn_split_kernel<T, CODE, D, NT, WAVES, true>), dim3((unsigned)(c.batch * c.heads_kv)), dim3(WAVES * 64), 0, a.stream, c, a.d, q,
+      hipLaunchKernelGGL((kv_attn_split_kernel<T, CODE, D, NT, WAVES, true>), dim3((unsigned)c.heads_kv, (unsigned)c.batch), dim3(WAVES * 64), 0, a.stream, c, a.d, q,
                          a.lengths, a.counts, out, a.lse, s);
       const ns_status st = check_launch("kv_attn_split_kernel");
       if (st != NS_OK || !again) return st;

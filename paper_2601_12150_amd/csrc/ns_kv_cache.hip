@@ -6,6 +6,7 @@ namespace ns {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostBlocks = 1 << 23;    // of one launch: a grid's threads along an axis are counted in 32 bits
 
 template <typename T> struct Row8;      // eight consecutive elements as they lie in memory
 template <> struct Row8<float> {
@@ -26,11 +27,12 @@ __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x
 // largest magnitude of all new values of the block: a thread has its up to PIECES times 8 in registers until it is known, so that they are
 // read once.  Bound by the reads and writes: 8404 tokens of 8 heads of 128 channels in bf16, 52 MB, 16 us (3.2 TB/s); one token 3.5 us.
 template <typename T, int CODE, int PIECES>
-__global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int tokens, const T *k, const T *v, int64_t sb, int64_t sh,
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int first, int tokens, const T *k, const T *v, int64_t sb, int64_t sh,
                                                              int64_t st, const int32_t *start, const int32_t *counts) {
   const int b = blockIdx.z, h = blockIdx.y >> 1, value = blockIdx.y & 1, tid = threadIdx.x;
   const int from = kv_length(start, b, c.capacity), to = min(from + kv_count(counts, b, tokens), c.capacity);
-  const int lblock = 31 - __clz(c.block), block = (from >> lblock) + (int)blockIdx.x, begin = block << lblock;
+  const int lblock = 31 - __clz(c.block), block = (from >> lblock) + first + (int)blockIdx.x, begin = block << lblock;
+  if (block >= c.capacity >> lblock) return;
   const int lo = max(from, begin), hi = min(to, begin + c.block);
   if (lo >= hi) return;
   const T *x = (value ? v : k) + b * sb + h * sh;
@@ -113,10 +115,12 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ns_kv_cache c, const 
 }
 
 template <typename T, int CODE>
-void append(const dim3 &grid, hipStream_t s, const ns_kv_cache &c, int tokens, const void *k, const void *v, int64_t sb, int64_t sh, int64_t st,
+void append(int blocks, hipStream_t s, const ns_kv_cache &c, int tokens, const void *k, const void *v, int64_t sb, int64_t sh, int64_t st,
             const int32_t *start, const int32_t *counts) {
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, c, tokens, static_cast<const T *>(k), static_cast<const T *>(v), sb, sh, st, start, counts);
+    for (int first = 0; first < blocks; first += kMostBlocks)
+      hipLaunchKernelGGL(kernel, dim3((unsigned)min(blocks - first, kMostBlocks), (unsigned)c.heads_kv * 2, (unsigned)c.batch), dim3(kThreads), 0, s, c, first,
+                         tokens, static_cast<const T *>(k), static_cast<const T *>(v), sb, sh, st, start, counts);
   };
   // what a thread has to hold: the block's values, or all the new ones
   const int values = (min(c.block, tokens) * c.head_dim + 8 * kThreads - 1) / (8 * kThreads);
@@ -129,13 +133,12 @@ ns_status launch_kv_append(const ns_kv_cache &c, int tokens, int dtype, const vo
                            int64_t st, const int32_t *start, const int32_t *counts, hipStream_t s) {
   // the blocks that so many tokens touch where they begin at a block's last position
   const int blocks = min((tokens + c.block - 2) / c.block + 1, c.capacity / c.block);
-  const dim3 grid((unsigned)blocks, (unsigned)c.heads_kv * 2, (unsigned)c.batch);
   if (dtype == NS_F32)
-    c.code == NS_CODE_I8 ? append<float, NS_CODE_I8>(grid, s, c, tokens, k, v, sb, sh, st, start, counts)
-                         : append<float, NS_CODE_E4M3>(grid, s, c, tokens, k, v, sb, sh, st, start, counts);
+    c.code == NS_CODE_I8 ? append<float, NS_CODE_I8>(blocks, s, c, tokens, k, v, sb, sh, st, start, counts)
+                         : append<float, NS_CODE_E4M3>(blocks, s, c, tokens, k, v, sb, sh, st, start, counts);
   else
-    c.code == NS_CODE_I8 ? append<bf16_t, NS_CODE_I8>(grid, s, c, tokens, k, v, sb, sh, st, start, counts)
-                         : append<bf16_t, NS_CODE_E4M3>(grid, s, c, tokens, k, v, sb, sh, st, start, counts);
+    c.code == NS_CODE_I8 ? append<bf16_t, NS_CODE_I8>(blocks, s, c, tokens, k, v, sb, sh, st, start, counts)
+                         : append<bf16_t, NS_CODE_E4M3>(blocks, s, c, tokens, k, v, sb, sh, st, start, counts);
   return check_launch("kv_append_kernel");
 }
 

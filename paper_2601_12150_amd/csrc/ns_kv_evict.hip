@@ -295,8 +295,8 @@ __global__ __launch_bounds__(kSelect) void kv_place_kernel(SelectArgs a, uint32_
 
 // One workgroup per block of the new cache, head, and keys or values; a thread has up to PIECES times 16 codes.
 template <int CODE, int PIECES, int THREADS>
-__global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_kv_cache to, const int32_t *lengths, const int32_t *kept, int keep) {
-  const int b = blockIdx.z, h = blockIdx.y >> 1, value = blockIdx.y & 1, tid = threadIdx.x, block = blockIdx.x;
+__global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_kv_cache to, const int32_t *lengths, const int32_t *kept, int keep, int first) {
+  const int b = blockIdx.z, h = blockIdx.y >> 1, value = blockIdx.y & 1, tid = threadIdx.x, block = first + (int)blockIdx.x;
   const int lo = block * to.block, here = min(to.block, min(kv_length(lengths, b, from.capacity), keep) - lo);
   if (here <= 0) return;
   const int64_t row = (int64_t)b * to.heads_kv + h;
@@ -357,8 +357,13 @@ __global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_k
 
 int chunks_of(int capacity) { return (capacity + kChunk - 1) / kChunk; }
 
-template <int CODE> void move(const dim3 &grid, hipStream_t s, const ns_kv_cache &from, const ns_kv_cache &to, const int32_t *lengths, const int32_t *kept, int keep) {
-  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, from, to, lengths, kept, keep); };
+template <int CODE> void move(hipStream_t s, const ns_kv_cache &from, const ns_kv_cache &to, const int32_t *lengths, const int32_t *kept, int keep) {
+  constexpr int kMost = 1 << 22;                      // blocks of one launch: a grid's threads along an axis are counted in 32 bits
+  auto go = [&](auto kernel, int threads) {
+    for (int first = 0, blocks = (keep + to.block - 1) / to.block; first < blocks; first += kMost)
+      hipLaunchKernelGGL(kernel, dim3((unsigned)min(blocks - first, kMost), (unsigned)to.heads_kv * 2, (unsigned)to.batch), dim3(threads), 0, s, from, to, lengths,
+                         kept, keep, first);
+  };
   switch (to.block * to.head_dim / 4096) {
     case 0: case 1: return go(kv_move_kernel<CODE, 1, 256>, 256);
     case 2: return go(kv_move_kernel<CODE, 2, 256>, 256);
@@ -392,8 +397,7 @@ ns_status launch_kv_evict(const ns_kv_cache &from, const ns_kv_cache &to, const 
     st = check_launch("kv_digit_kernel / kv_place_kernel");
   }
   if (st != NS_OK) return st;
-  const dim3 grid((unsigned)((keep + to.block - 1) / to.block), (unsigned)to.heads_kv * 2, (unsigned)to.batch);
-  to.code == NS_CODE_I8 ? move<NS_CODE_I8>(grid, s, from, to, lengths, kept, keep) : move<NS_CODE_E4M3>(grid, s, from, to, lengths, kept, keep);
+  to.code == NS_CODE_I8 ? move<NS_CODE_I8>(s, from, to, lengths, kept, keep) : move<NS_CODE_E4M3>(s, from, to, lengths, kept, keep);
   return check_launch("kv_move_kernel");
 }
 

@@ -33,3 +33,52 @@ def test_attention_where_all_logits_are_low(nb, dtype, code, D, G, T, low):
     want = oracle.attend(q, oracle.values(host[0], host[1]), oracle.values(host[2], host[3]), [N, 333], [T] * B, float(np.float32(D ** -0.5)), True)
     assert want[1][np.isfinite(want[1])].min() < 20 - low
     check_attention(*got, want, dtype, D, N, G * T)
+
+
+def test_more_heads_than_a_grid_has_threads_for_along_an_axis(nb):
+    """65535 sequences of 256 heads, which share what they hold, each with a workgroup to itself."""
+    B, H, N, D = 65535, 256, 32, 64
+    rng = np.random.default_rng(4)
+    one, _ = make(nb, rng, 1, 1, N, D, 32, "i8", [N])
+    cache = nb.kv_cache(one.k.expand(B, H, -1, -1), one.v.expand(B, H, -1, -1), one.k_scale.expand(B, H, -1).contiguous(), one.v_scale.expand(B, H, -1).contiguous())
+    q = torch.randn((1, 1, 1, D), device="cuda").to(torch.bfloat16)
+    lengths = torch.arange(B, device="cuda", dtype=torch.int32) % 33
+    got = nb.kv_cache_attn(cache, q.expand(B, H, -1, -1), lengths)
+    want = torch.cat([nb.kv_cache_attn(one, q, i32([n])) for n in range(33)])[:, 0, 0]
+    for b in range(0, B, 4096):
+        assert torch.equal(got[b:b + 4096, :, 0], want[lengths[b:b + 4096].long()][:, None].expand(-1, H, -1))
+
+
+def test_more_blocks_than_a_grid_has_threads_for_along_an_axis(nb):
+    """2^29 tokens in blocks of 32 enter a cache and move to another one."""
+    N, D, block = 1 << 29, 64, 32
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GiB of free memory")
+    rng = np.random.default_rng(2)
+    at = [slice(0, 64), slice((1 << 28) - 64, (1 << 28) + 64), slice(N - 64, N)]
+    x = torch.empty((1, 1, N, D), device="cuda", dtype=torch.bfloat16)
+    for j, a in enumerate(at):
+        x[:, :, a] = dev(rng.standard_normal((1, 1, a.stop - a.start, D)) * 4.0 ** j, torch.bfloat16)
+    raw = [torch.empty((1, 1, N, D), device="cuda", dtype=torch.int8) for _ in range(2)]
+    scale = [torch.empty((1, 1, N // block), device="cuda") for _ in range(2)]
+    cache = nb.kv_cache(*raw, *scale)
+    nb.kv_cache_append(cache, x, x, i32([0]))
+    small = nb.kv_cache_empty(1, 1, 256, D, block)
+    nb.kv_cache_append(small, *[torch.cat([x[:, :, a] for a in at], 2)] * 2, i32([0]))
+    del x
+    torch.cuda.empty_cache()
+
+    def check(c):
+        for i in range(4):
+            per = block if i >= 2 else 1
+            got = torch.cat([c[i][:, :, a.start // per:a.stop // per] for a in at], 2)
+            assert torch.equal(got, small[i])
+
+    check(cache)
+    to = nb.kv_cache(*(torch.empty_like(r) for r in raw), *(torch.empty_like(s) for s in scale))
+    kept, _, left = nb.kv_cache_evict(cache, to, torch.zeros((1, 1, N), device="cuda"), i32([N]), N)
+    assert left.item() == N and all(kept[0, 0, a].tolist() == list(range(a.start, a.stop)) for a in at)
+    check(to)
+    del cache, to, raw, scale, kept
+    torch.cuda.empty_cache()
