@@ -76,6 +76,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int 
     }
   }
   const bool plain = kv_is_pow2(s);                                    // else one of the caller's own: the quotient is rounded, then the code
+  const bool none = kv_is_nan(s) || s == 0.f;                          // (0: the caller's own for a block of zeros, which zeros have entered)
   const float inv = plain ? 1.f / s : 1.f;
 #pragma unroll
   for (int i = 0; i < PIECES; i++) {
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int 
       for (int j = 0; j < 2; j++) {
         f32x4 z = y[i].half(j);
         if (!plain) z /= s;
-        w[j] = kv_is_nan(s) ? 0u : kv_encode4<CODE>(z, inv);
+        w[j] = none ? 0u : kv_encode4<CODE>(z, inv);
       }
       *reinterpret_cast<u32x2 *>(codes + n * c.stride_t + d) = w;
     }

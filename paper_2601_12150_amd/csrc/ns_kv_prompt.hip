@@ -175,7 +175,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
   float unit = 0.f, next = 0.f, inv_next = 0.f, rel0 = 0.f, rel1 = 0.f;
   bool slow = true;
   // (branches, both here and for the last tile: 262 -> 244 us for the prompts of 2 x 4096 tokens)
-  uint32_t last_bits0 = 0, last_bits1 = 0;          // the scales that these go by; 0 is none
+  uint32_t last_bits0 = 0, last_bits1 = 0;          // the scales that these go by; 0 for none, which have what scales of 0 would make of them
   By<CODE> v_by[VP];
 #pragma unroll
   for (int i = 0; i < VP; i++) v_by[i] = kv_by<CODE>(1.f);
@@ -316,7 +316,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
         for (int e = 0; e < 16; e++) s[x][e] -= move;
       if (moved) m = ref + move;
       l *= fade;
-      fade *= unit / tile_unit;
+      if (tile_unit != unit) fade *= unit / tile_unit;     // (both are 0 as long as all scales were 0 or NaN)
       unit = tile_unit;
 #pragma unroll
       for (int i = 0; i < MT; i++) o[i] *= fade;

@@ -82,3 +82,53 @@ def test_more_blocks_than_a_grid_has_threads_for_along_an_axis(nb):
     check(to)
     del cache, to, raw, scale, kept
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("zero", ["first", "some", "all"])
+@pytest.mark.parametrize("dtype,code,D,G,T", [("bf16", "i8", 64, 2, 1), ("f32", "e4m3", 128, 4, 4), ("bf16", "i8", 64, 2, 200), ("bf16", "e4m3", 128, 2, 200),
+                                              ("f32", "i8", 128, 1, 150), ("bf16", "i8", 256, 1, 90), ("f32", "e4m3", 256, 2, 90)])
+def test_attention_to_blocks_of_scale_0(nb, dtype, code, D, G, T, zero):
+    """A caller's own quantisation gives a block of zeros the scale 0: its tokens are zeros, whatever their codes."""
+    B, H, block, N = 2, 2, 32, 608
+    rng = np.random.default_rng(D + T)
+    cache, host = make(nb, rng, B, H, N, D, block, code, [N, 333])
+    blocks = {"first": [0, 1, 2, 3], "some": [4, 5, 9], "all": list(range(N // block))}[zero]
+    for i in (1, 3):
+        host[i] = rng.uniform(0.001, 0.02, host[i].shape).astype(np.float32).astype(np.float64)
+        host[i][:, :, blocks] = 0.0
+    host[1][0, 0] = 0.01                                         # one head has zeros among its values only
+    cache = cache._replace(k_scale=dev(host[1], torch.float32), v_scale=dev(host[3], torch.float32))
+    host[1], host[3] = f64(cache.k_scale), f64(cache.v_scale)
+    key, value = oracle.values(host[0], host[1]), oracle.values(host[2], host[3])
+    q = rounded((rng.standard_normal((B, H * G, T, D)) * 3).astype(np.float32), dtype)
+    got = nb.kv_cache_attn(cache, dev(q, DTYPES[dtype]), i32([N, 333]), want_lse=True, want_weights=True)
+    check_attention(*got, oracle.attend(q, key, value, [N, 333], [T] * B, float(np.float32(D ** -0.5)), True), dtype, D, N, G * T)
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_append_to_and_evict_from_blocks_of_scale_0(nb, code):
+    """Zeros that enter a block of scale 0 leave it one; others give it their scale."""
+    rng = np.random.default_rng(1)
+    B, H, N, D, block = 1, 2, 128, 64, 32
+    cache, host = make(nb, rng, B, H, N, D, block, code, [N])
+    for i in (1, 3):
+        host[i][:, :, [0, 2]] = 0.0
+    cache = cache._replace(k_scale=dev(host[1], torch.float32), v_scale=dev(host[3], torch.float32))
+    zeros, ones = np.zeros((1, H, 3, D)), np.ones((1, H, 3, D))
+    for at, x, y in ((5, zeros, zeros), (70, zeros, ones)):
+        nb.kv_cache_append(cache, dev(x, torch.float32), dev(y, torch.float32), i32([at]))
+        for i, new in ((0, x), (2, y)):
+            if not new.any():
+                host[i][:, :, at:at + 3] = 0.0                   # (the scale stays 0)
+            else:
+                oracle.append(host[i], host[i + 1], new, [at], [3], code)
+    check_same(cache, host)
+    assert all(torch.isfinite(c.float()).all() for c in cache[:2])
+    w = rng.uniform(0, 1, (B, H, N)).astype(np.float32)
+    to = nb.kv_cache_empty(B, H, 64, D, block, CODES[code])
+    nb.kv_cache_evict(cache, to, dev(w), i32([N]), 50)
+    for h in range(H):
+        kept = oracle.select(w[0, h], N, 50, 1, 0)
+        for codes, scale, i in ((to.k, to.k_scale, 0), (to.v, to.v_scale, 2)):
+            ref, ref_scale = oracle.move(host[i][0, h], host[i + 1][0, h], kept, block, code)
+            assert np.array_equal(f64(codes[0, h]), ref) and np.array_equal(f64(scale[0, h]), ref_scale)
