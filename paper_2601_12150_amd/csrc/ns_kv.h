@@ -65,6 +65,25 @@ __device__ __forceinline__ uint32_t kv_encode4(f32x4 x, float f) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, w, true);
 }
 
+// a power of two (whose reciprocal is one too), or 0
+__device__ __forceinline__ bool kv_is_pow2(float s) { return (__float_as_uint(s) & 0x7fffffu) == 0; }
+
+// x * f for a rounding to far fewer bits that is the only one: of a product that fp32 does not hold, the neighbour whose last bit is 1.  No
+// border between codes has that bit, so that the product lies on the same side of all of them.
+__device__ __forceinline__ float kv_mul_odd(float x, float f) {
+  const float p = x * f, off = __builtin_fmaf(x, f, -p);               // (off: exact)
+  const uint32_t u = __float_as_uint(p);
+  return off == 0.f || (u & 1u) ? p : __uint_as_float((off < 0.f) == (p < 0.f) ? u + 1 : u - 1);
+}
+// The nearest codes of codes times any ratio f.  (int8's rounding in kv_encode4 is one already.)
+template <int CODE> __device__ __forceinline__ uint32_t kv_recode4(uint32_t w, float f) {
+  f32x4 x = kv_decode4<CODE>(w);
+  if (CODE == NS_CODE_I8 || kv_is_pow2(f)) return kv_encode4<CODE>(x, f);
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = kv_mul_odd(x[i], f);
+  return kv_encode4<CODE>(x, 1.f);
+}
+
 template <int CODE> __device__ __forceinline__ constexpr float kv_limit() { return CODE == NS_CODE_I8 ? 127.f : 448.f; }   // the largest code
 constexpr uint32_t kInfBits = 0x7f800000u, kNanBits = 0x7fc00000u;
 // The scale of a block whose largest magnitude has these bits: 2^e, e the smallest with most <= 127 * 2^e (448 * 2^e), at
@@ -77,8 +96,6 @@ __device__ __forceinline__ float kv_scale_for(uint32_t most) {
   const int e = CODE == NS_CODE_I8 ? x - 6 + (f > 0x7e0000) : x - 8 + (f > 0x600000);
   return __uint_as_float((uint32_t)(max(e, -100) + 127) << 23);
 }
-// a power of two (whose reciprocal is one too)
-__device__ __forceinline__ bool kv_is_pow2(float s) { return (__float_as_uint(s) & 0x7fffffu) == 0; }
 __device__ __forceinline__ bool kv_is_nan(float s) { return !(s == s); }
 
 // ---- matrix products over codes

@@ -66,13 +66,14 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(ns_kv_cache c, int 
   most = max(max(largest[0], largest[1]), max(largest[2], largest[3]));
   float s = kv_scale_for<CODE>(most);
   // (the comparison is false for a NaN on either side: a NaN block stays one, a NaN among the new tokens makes it one)
-  if (live && (kv_is_nan(old) || (most < kInfBits && __uint_as_float(most) <= kv_limit<CODE>() * old))) s = old;
+  // (the sign of limit * old - most is exact this way)
+  if (live && (kv_is_nan(old) || (most < kInfBits && __builtin_fmaf(kv_limit<CODE>(), old, -__uint_as_float(most)) >= 0.f))) s = old;
   if (live && s > old) {                                               // (not with a NaN: the codes no longer matter)
     const float ratio = old / s;
     for (int n = begin + (tid >> lpieces); n < from; n += step) {
       u32x2 *w = reinterpret_cast<u32x2 *>(codes + n * c.stride_t + d);
       const u32x2 was = *w;
-      *w = u32x2{kv_encode4<CODE>(kv_decode4<CODE>(was[0]), ratio), kv_encode4<CODE>(kv_decode4<CODE>(was[1]), ratio)};
+      *w = u32x2{kv_recode4<CODE>(was[0], ratio), kv_recode4<CODE>(was[1], ratio)};
     }
   }
   const bool plain = kv_is_pow2(s);                                    // else one of the caller's own: the quotient is rounded, then the code

@@ -329,7 +329,8 @@ __global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_k
       top = fmaxf(fmaxf(top, fmaxf(__builtin_fabsf(c[0]), __builtin_fabsf(c[1]))), fmaxf(__builtin_fabsf(c[2]), __builtin_fabsf(c[3])));
     }
     nan |= kv_is_nan(scale[i]);
-    most = fmaxf(most, top * scale[i]);
+    const float x = top * scale[i], off = __builtin_fmaf(top, scale[i], -x);
+    most = fmaxf(most, off > 0.f ? __uint_as_float(__float_as_uint(x) + 1) : x);     // (rounded up: not to the limit of a scale below)
   }
   __shared__ float largest[THREADS / 64];
   if (nan) most = INFINITY;
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_k
     if (scale[i] != s && t < here) {
       const float ratio = scale[i] / s;               // (exact: s is a power of two)
 #pragma unroll
-      for (int j = 0; j < 4; j++) w[j] = kv_is_nan(s) ? 0u : kv_encode4<CODE>(kv_decode4<CODE>(w[j]), ratio);
+      for (int j = 0; j < 4; j++) w[j] = kv_is_nan(s) ? 0u : kv_recode4<CODE>(w[j], ratio);
     }
     *reinterpret_cast<u32x4 *>(dst + (int64_t)(lo + t) * to.stride_t) = w;
   }

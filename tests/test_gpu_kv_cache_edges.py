@@ -132,3 +132,96 @@ def test_append_to_and_evict_from_blocks_of_scale_0(nb, code):
         for codes, scale, i in ((to.k, to.k_scale, 0), (to.v, to.v_scale, 2)):
             ref, ref_scale = oracle.move(host[i][0, h], host[i + 1][0, h], kept, block, code)
             assert np.array_equal(f64(codes[0, h]), ref) and np.array_equal(f64(scale[0, h]), ref_scale)
+
+
+def scale_beside_a_tie(code, tie):
+    """A scale of 24 bits whose product with `code` (1 to 15) is next to `tie` (an odd number of 5 bits: half way between two of e4m3's) times
+    2^23, nearer than fp32 can tell: (scale below 2, of the tie's own unit; the product's distance in units of 2^-23)."""
+    for off in (1, -1, 2, -2, 3, -3, 5, -5, 7, -7):
+        if (tie * 2 ** 23 + off) % code == 0:
+            m = (tie * 2 ** 23 + off) // code
+            while m >= 2 ** 24 and m % 2 == 0:
+                m //= 2
+            if 2 ** 23 <= m < 2 ** 24 and abs(off) * 2.0 ** -23 < tie * 2.0 ** -24:
+                return m * 2.0 ** -23
+    return None
+
+
+def near_ties():
+    """(code, scale): products that are no ties but round to one in fp32."""
+    found = []
+    for code in range(8, 16):
+        for tie in range(17, 32, 2):
+            s = scale_beside_a_tie(code, tie)
+            if s is not None and float(np.float32(code * s)) != code * s and float(np.float32(code * s) * 2.0 ** 23) % 2 ** 19 == 0:
+                found.append((code, s))
+    return found
+
+
+def test_moved_codes_are_rounded_once(nb):
+    """Values of the caller's own scales that are no ties, but of which fp32 makes one: the nearest code is told by what fp32 drops."""
+    pairs = near_ties()
+    assert len(pairs) >= 8
+    block, D, N = 32, 64, 32 * len(pairs)
+    codes, scale = np.zeros((1, 1, N, D)), np.zeros((1, 1, len(pairs)))
+    for j, (c, s) in enumerate(pairs):
+        codes[0, 0, j * block:(j + 1) * block] = np.random.default_rng(j).integers(-c, c + 1, (block, D))
+        codes[0, 0, j * block:j * block + 2] = np.array([[c], [-c]])
+        scale[0, 0, j] = s
+    put = torch.from_numpy(codes).float().to(torch.float8_e4m3fn).cuda()
+    cache = nb.kv_cache(put, put.clone(), dev(scale, torch.float32), dev(scale, torch.float32))
+    to = nb.kv_cache_empty(1, 1, N, D, block, torch.float8_e4m3fn)
+    nb.kv_cache_evict(cache, to, torch.zeros((1, 1, N), device="cuda"), i32([N]), N)
+    ref, ref_scale = oracle.move(codes[0, 0], scale[0, 0], np.arange(N), block, "e4m3")
+    assert np.array_equal(f64(to.k_scale[0, 0]), ref_scale) and np.array_equal(f64(to.k[0, 0]), ref) and np.array_equal(f64(to.v[0, 0]), ref)
+    # one token that needs a larger scale: what the block held is rounded again
+    host = [codes, scale, codes.copy(), scale.copy()]
+    for j in range(len(pairs)):
+        x = np.full((1, 1, 1, D), 2.0 ** 11)
+        nb.kv_cache_append(cache, dev(x, torch.float32), dev(x, torch.float32), i32([j * block + block - 1]))
+        for i in (0, 2):
+            oracle.append(host[i], host[i + 1], x, [j * block + block - 1], [1], "e4m3")
+    check_same(cache, host)
+
+
+@pytest.mark.parametrize("code,limit", [("i8", 127), ("e4m3", 448)])
+def test_scales_beside_their_limits(nb, code, limit):
+    """A block's largest value is beside the limit of a scale by less than fp32 can tell: the smallest scale that holds it is still meant."""
+    found = []
+    for c in range(1, 128 if code == "i8" else 16):
+        m = round(limit * 2.0 ** 23 / c)
+        for m in (m, m + 1):
+            while m >= 2 ** 24:
+                m //= 2
+            while m < 2 ** 23:
+                m *= 2
+            s = m * 2.0 ** -23
+            ratio = c * s / limit
+            while ratio > 1.5:
+                ratio /= 2
+            while ratio < 0.75:
+                ratio *= 2
+            if 1 < ratio < 1 + 2.0 ** -24 or 1 - 2.0 ** -24 < ratio < 1:
+                found.append((c, s))
+    assert len(found) >= 4
+    block, D, N = 32, 64, 32 * len(found)
+    codes, scale = np.zeros((1, 1, N, D)), np.zeros((1, 1, len(found)))
+    for j, (c, s) in enumerate(found):
+        codes[0, 0, j * block + 3, 5] = -c
+        scale[0, 0, j] = s
+    put = torch.from_numpy(codes).float().to(CODES[code]).cuda()
+    cache = nb.kv_cache(put, put.clone(), dev(scale, torch.float32), dev(scale, torch.float32))
+    to = nb.kv_cache_empty(1, 1, N, D, block, CODES[code])
+    nb.kv_cache_evict(cache, to, torch.zeros((1, 1, N), device="cuda"), i32([N]), N)
+    ref, ref_scale = oracle.move(codes[0, 0], scale[0, 0], np.arange(N), block, code)
+    assert np.array_equal(f64(to.k_scale[0, 0]), ref_scale) and np.array_equal(f64(to.k[0, 0]), ref)
+    # a new token of just that size, and the floats next to it, in a block of such a scale
+    for c, s in found:
+        for x in (np.float32(limit * s), np.nextafter(np.float32(limit * s), np.float32(0)), np.nextafter(np.float32(limit * s), np.float32(1e9))):
+            host = [np.zeros((1, 1, block, D)), np.full((1, 1, 1), s)]
+            one = nb.kv_cache_empty(1, 1, block, D, block, CODES[code])
+            one.k_scale.fill_(s), one.v_scale.fill_(s)
+            new = np.full((1, 1, 1, D), float(x))
+            nb.kv_cache_append(one, dev(new, torch.float32), dev(new, torch.float32), i32([4]))
+            oracle.append(*host, new, [4], [1], code)
+            assert one.k_scale.item() == host[1].item() and np.array_equal(f64(one.k), host[0])
