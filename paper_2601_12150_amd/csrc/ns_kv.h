@@ -201,7 +201,7 @@ __device__ __forceinline__ void kv_rows_tile(const ns_kv_cache &c, const ns_kv_a
   most = max(most, (uint32_t)__shfl_xor((int)most, 16));
   most = max(most, (uint32_t)__shfl_xor((int)most, 32));
   const int shift = kv_row_shift(most);
-  if (g == 0) factors[row * tiles * 16 + r] = real ? ldexpf(d.scale * kLog2e, -shift) : 0.f;
+  if (g == 0) factors[row * tiles * 16 + r] = real ? ldexpf(d.scale, -shift) * kLog2e : 0.f;
   for (int s = 0; s < KS; s++) {
     Frag f[PARTS];
 #pragma unroll

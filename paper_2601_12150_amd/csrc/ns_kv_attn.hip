@@ -250,7 +250,7 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
       most = max(most, (uint32_t)__shfl_xor((int)most, 16));
       most = max(most, (uint32_t)__shfl_xor((int)most, 32));
       const int shift = kv_row_shift(most);
-      factor[nt] = ldexpf(d.scale * kLog2e, -shift);
+      factor[nt] = ldexpf(d.scale, -shift) * kLog2e;
 #pragma unroll
       for (int i = 0; i < D / 16; i++)
 #pragma unroll

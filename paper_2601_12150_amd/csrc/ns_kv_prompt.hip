@@ -144,7 +144,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
       }
     most = max(most, (uint32_t)__shfl_xor((int)most, 32));
     const int shift = kv_row_shift(most);
-    factor = real ? ldexpf(d.scale * kLog2e, -shift) : 0.f;
+    factor = real ? ldexpf(d.scale, -shift) * kLog2e : 0.f;
 #pragma unroll
     for (int s = 0; s < KS; s++)
 #pragma unroll

@@ -225,3 +225,17 @@ def test_scales_beside_their_limits(nb, code, limit):
             nb.kv_cache_append(one, dev(new, torch.float32), dev(new, torch.float32), i32([4]))
             oracle.append(*host, new, [4], [1], code)
             assert one.k_scale.item() == host[1].item() and np.array_equal(f64(one.k), host[0])
+
+
+@pytest.mark.parametrize("T", [1, 12, 70])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_the_largest_scales(nb, dtype, T):
+    """A scale near the end of fp32's range, whose product with log2 e is beyond it, and queries as small as that takes."""
+    D, N = 64, 256
+    rng = np.random.default_rng(9)
+    cache, host = make(nb, rng, 1, 1, N, D, 64, "i8", [N])
+    q = rounded((rng.standard_normal((1, 2, T, D)) * 2.0 ** -131).astype(np.float32), dtype)
+    scale = float(np.float32(3e38))
+    got = nb.kv_cache_attn(cache, dev(q, DTYPES[dtype]), i32([N]), scale=scale, want_lse=True, want_weights=True)
+    want = oracle.attend(q, oracle.values(host[0], host[1]), oracle.values(host[2], host[3]), [N], [T], scale, True)
+    check_attention(*got, want, dtype, D, N, 2 * T)
