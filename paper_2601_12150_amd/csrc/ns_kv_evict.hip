@@ -5,7 +5,8 @@
 // 11 and 10 bits, each from a histogram of the keys that share the digits before it (radix select).  Then all tokens with a larger
 // key stay, and of those with this very key the first ones.
 //   kv_select_kernel: caches of up to 16384 tokens; one workgroup per sequence and head has all keys in registers, one launch.
-//   kv_digit_kernel, kv_place_kernel: longer ones, a workgroup per 8192 tokens; a launch for every digit and one that places.
+//   kv_digit_kernel, kv_place_kernel: longer ones, a workgroup per 8192 tokens, or as many times that as leave 64 of them; a launch for every digit
+//     and one that places.
 //   kv_move_kernel: a workgroup per block of the new cache; its codes are read once and stay in registers until the scale is known.
 // Measured: selection among 577 tokens 7.6 us, among 16000 (64 sequences and heads) 23 us, both bound by the barriers between the passes; among
 // 131001 (8 heads) 7 + 9 + 9 + 12 us, bound by launches and the sums over all workgroups' histograms.  The move: 32768 tokens of 8 heads of 128
@@ -21,7 +22,11 @@ constexpr int kBits[3] = {11, 11, 10}, kShift[3] = {21, 10, 0}, kBins = 2048;
 // Tokens that one workgroup selects from: 8 heads' 16384 to 1000 take 21 us with, 31 without (the move included); one of 32768 would take
 // 34 against 32.
 constexpr int kHeld = 16384;
-constexpr int kChunkKeys = 8, kChunk = kSelect * kChunkKeys;
+constexpr int kChunkKeys = 8, kPiece = kSelect * kChunkKeys;
+// Chunks of a sequence and head, each with a workgroup and one piece or several: every workgroup reads all chunks' histograms, which without
+// an end to their number would be work that grows with the square of the capacity (8 heads' 2^20 tokens to 4096: 119 us, 259 with a workgroup
+// for every piece; 2^22: 244 and 3206).
+constexpr int kMostChunks = 64;
 
 // larger weight <=> larger key; -0 and +0 alike, NaN above everything
 __device__ __forceinline__ uint32_t rank_key(float w) {
@@ -61,6 +66,7 @@ struct SelectArgs {
   const float *weights;
   const int32_t *lengths;
   int capacity, keep, n_global, n_recent, heads_kv, to_capacity;
+  int pieces;                                     // of a chunk
   int32_t *kept;
   float *w_out;
   int32_t *lengths_out;
@@ -80,10 +86,11 @@ __device__ __forceinline__ bool all_stay(const SelectArgs &a, int64_t row, int l
 }
 
 // Writes the tokens that stay of KPT * 1024 tokens from `base`: thread's token i is base + wave * 64 KPT + 64 i + lane.  placed, equal: how
-// many stay, and how many have the border's key, before these.
+// many stay, and how many have the border's key, before these; those of these are added where more follow.
 template <int KPT>
 __device__ __forceinline__ void place(const SelectArgs &a, int64_t row, const float *w, const uint32_t (&key)[KPT], int base, int length,
-                                      uint32_t border, uint32_t need, bool ranked, uint32_t placed, uint32_t equal, int tid, uint32_t *shared /* [2 kWaves] */) {
+                                      uint32_t border, uint32_t need, bool ranked, uint32_t &placed, uint32_t &equal, bool more, int tid,
+                                      uint32_t *shared /* [2 kWaves] */) {
   const int lane = tid & 63, wave = tid >> 6;
   const int first = a.n_global, last = length - a.n_recent;
   const unsigned long long below = (1ull << lane) - 1;
@@ -101,13 +108,16 @@ __device__ __forceinline__ void place(const SelectArgs &a, int64_t row, const fl
     shared[kWaves + wave] = eqs;
   }
   __syncthreads();
-  uint32_t sure_before = 0;
+  // all tokens before this wave that stay: the sure ones, and of those with the border's key the first `need`
+  uint32_t at = placed, eq = equal;
   for (int x = 0; x < wave; x++) {
-    sure_before += shared[x];
+    at += shared[x];
+    eq += shared[kWaves + x];
+  }
+  for (int x = 0; more && x < kWaves; x++) {
+    placed += shared[x];
     equal += shared[kWaves + x];
   }
-  // all tokens before this wave that stay: the sure ones, and of those with the border's key the first `need`
-  uint32_t at = placed + sure_before, eq = equal;
 #pragma unroll
   for (int i = 0; i < KPT; i++) {
     const int n = n0 + 64 * i;
@@ -162,7 +172,8 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(SelectArgs a) {
       need = c.need;
     }
   }
-  place<KPT>(a, row, w, key, 0, length, prefix, need, ranked, 0, 0, tid, shared);
+  uint32_t placed = 0, equal = 0;
+  place<KPT>(a, row, w, key, 0, length, prefix, need, ranked, placed, equal, false, tid, shared);
 }
 
 // ---- longer caches.  Scratch of a sequence and head: a histogram for every digit and chunk, the border's digits so far, and how many of each
@@ -176,6 +187,13 @@ inline __host__ __device__ size_t scratch_words(int chunks) { return (size_t)3 *
 __device__ __forceinline__ Scratch scratch_of(uint32_t *ws, int64_t row, int chunks) {
   uint32_t *p = ws + row * scratch_words(chunks);
   return Scratch{p, p + (size_t)3 * chunks * kBins, p + (size_t)3 * chunks * kBins + 8};
+}
+
+// The keys of a piece, in the places that place() has them
+__device__ __forceinline__ void load_keys(const float *w, int base, int length, int wave, int lane, uint32_t (&key)[kChunkKeys]) {
+  const int n0 = base + wave * 64 * kChunkKeys + lane;
+#pragma unroll
+  for (int i = 0; i < kChunkKeys; i++) key[i] = n0 + 64 * i < length ? rank_key(w[n0 + 64 * i]) : 0u;
 }
 
 // Sums over the workgroup
@@ -233,10 +251,9 @@ __global__ __launch_bounds__(kSelect) void kv_digit_kernel(SelectArgs a, uint32_
   const float *w = a.weights + row * a.capacity;
   __shared__ __attribute__((aligned(8))) uint32_t hist[kBins];
   __shared__ uint32_t shared[2 * kWaves + 3];
-  const int first = a.n_global, last = length - a.n_recent, n0 = chunk * kChunk + wave * 64 * kChunkKeys + lane;
+  const int first = a.n_global, last = length - a.n_recent, lo = chunk * a.pieces * kPiece, hi = min(lo + a.pieces * kPiece, length);
   uint32_t key[kChunkKeys];
-#pragma unroll
-  for (int i = 0; i < kChunkKeys; i++) key[i] = n0 + 64 * i < length ? rank_key(w[n0 + 64 * i]) : 0u;
+  load_keys(w, lo, length, wave, lane, key);
   *reinterpret_cast<u32x2 *>(&hist[2 * tid]) = u32x2{0, 0};
   uint32_t prefix = 0;
   if (PASS > 0) {
@@ -249,9 +266,13 @@ __global__ __launch_bounds__(kSelect) void kv_digit_kernel(SelectArgs a, uint32_
   }
   __syncthreads();
   const uint32_t mask = PASS == 0 ? 0u : ~0u << kShift[PASS > 0 ? PASS - 1 : 0];
+  for (int base = lo; base < hi; base += kPiece) {
+    if (base > lo) load_keys(w, base, length, wave, lane, key);
+    const int n0 = base + wave * 64 * kChunkKeys + lane;
 #pragma unroll
-  for (int i = 0; i < kChunkKeys; i++)
-    if (n0 + 64 * i >= first && n0 + 64 * i < last && (key[i] & mask) == prefix) atomicAdd(&hist[digit_of(key[i], PASS)], 1u);
+    for (int i = 0; i < kChunkKeys; i++)
+      if (n0 + 64 * i >= first && n0 + 64 * i < last && (key[i] & mask) == prefix) atomicAdd(&hist[digit_of(key[i], PASS)], 1u);
+  }
   __syncthreads();
   *reinterpret_cast<u32x2 *>(s.hist + ((size_t)PASS * chunks + chunk) * kBins + 2 * tid) = *reinterpret_cast<const u32x2 *>(&hist[2 * tid]);
 }
@@ -266,13 +287,11 @@ __global__ __launch_bounds__(kSelect) void kv_place_kernel(SelectArgs a, uint32_
   const uint32_t need0 = (uint32_t)(a.keep - a.n_global - a.n_recent);
   const bool ranked = need0 > 0;
   __shared__ uint32_t shared[2 * kWaves + 3];
-  const int first = a.n_global, last = length - a.n_recent, lo = chunk * kChunk;
-  if (lo >= length) return;
+  const int first = a.n_global, last = length - a.n_recent, lo = chunk * a.pieces * kPiece, hi = min(lo + a.pieces * kPiece, length);
+  if (lo >= hi) return;
   uint32_t prefix = 0, need = 0, placed = 0, equal = 0;
-  const int n0 = lo + wave * 64 * kChunkKeys + lane;
   uint32_t key[kChunkKeys];
-#pragma unroll
-  for (int i = 0; i < kChunkKeys; i++) key[i] = n0 + 64 * i < length ? rank_key(w[n0 + 64 * i]) : 0u;
+  load_keys(w, lo, length, wave, lane, key);
   if (ranked) {
     const Scratch s = scratch_of(ws, row, chunks);
     u32x2 own, before;
@@ -288,7 +307,13 @@ __global__ __launch_bounds__(kSelect) void kv_place_kernel(SelectArgs a, uint32_
   }
   placed += (uint32_t)(min(lo, first) + max(0, min(lo, length) - max(last, 0)));      // and those that stay in any case
   // (place() counts tokens with the border's key from `equal` on; those of them before that stay are the first `need`)
-  place<kChunkKeys>(a, row, w, key, lo, length, prefix, need, ranked, placed, equal, tid, shared);
+  for (int base = lo; base < hi; base += kPiece) {
+    if (base > lo) {
+      __syncthreads();
+      load_keys(w, base, length, wave, lane, key);
+    }
+    place<kChunkKeys>(a, row, w, key, base, length, prefix, need, ranked, placed, equal, base + kPiece < hi, tid, shared);
+  }
 }
 
 // ---- the move
@@ -356,7 +381,8 @@ __global__ __launch_bounds__(THREADS) void kv_move_kernel(ns_kv_cache from, ns_k
   if (tid == 0) (value ? to.v_scale : to.k_scale)[row * (to.capacity / to.block) + block] = s;
 }
 
-int chunks_of(int capacity) { return (capacity + kChunk - 1) / kChunk; }
+int pieces_of(int capacity) { return ((capacity + kPiece - 1) / kPiece + kMostChunks - 1) / kMostChunks; }
+int chunks_of(int capacity) { return ((capacity + kPiece - 1) / kPiece + pieces_of(capacity) - 1) / pieces_of(capacity); }
 
 template <int CODE> void move(hipStream_t s, const ns_kv_cache &from, const ns_kv_cache &to, const int32_t *lengths, const int32_t *kept, int keep) {
   constexpr int kMost = 1 << 22;                      // blocks of one launch: a grid's threads along an axis are counted in 32 bits
@@ -381,7 +407,7 @@ size_t kv_evict_workspace_bytes(const ns_kv_cache &from, int) {
 
 ns_status launch_kv_evict(const ns_kv_cache &from, const ns_kv_cache &to, const float *weights, const int32_t *lengths, int keep,
                           int n_global, int n_recent, int32_t *kept, float *w_out, int32_t *lengths_out, void *ws, hipStream_t s) {
-  const SelectArgs a{weights, lengths, from.capacity, keep, n_global, n_recent, from.heads_kv, to.capacity, kept, w_out, lengths_out};
+  const SelectArgs a{weights, lengths, from.capacity, keep, n_global, n_recent, from.heads_kv, to.capacity, pieces_of(from.capacity), kept, w_out, lengths_out};
   ns_status st;
   if (from.capacity <= kHeld) {
     const dim3 grid((unsigned)from.heads_kv, (unsigned)from.batch);

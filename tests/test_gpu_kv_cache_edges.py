@@ -239,3 +239,37 @@ def test_attention_of_the_largest_scales(nb, dtype, T):
     got = nb.kv_cache_attn(cache, dev(q, DTYPES[dtype]), i32([N]), scale=scale, want_lse=True, want_weights=True)
     want = oracle.attend(q, oracle.values(host[0], host[1]), oracle.values(host[2], host[3]), [N], [T], scale, True)
     check_attention(*got, want, dtype, D, N, 2 * T)
+
+
+def select(w, length, keep, n_global, n_recent):
+    """oracle.select for weights without NaN, by a stable sort."""
+    if length <= keep:
+        return np.arange(length)
+    order = np.argsort(-w[n_global:length - n_recent].astype(np.float64), kind="stable")[:keep - n_global - n_recent] + n_global
+    return np.sort(np.concatenate([np.arange(n_global), order, np.arange(length - n_recent, length)]))
+
+
+@pytest.mark.parametrize("N,lengths", [(1 << 19, [1 << 19, 524000]), ((1 << 19) + 64, [(1 << 19) + 64, 500001, 8193]), (1700032, [1700001, 300000])])
+@pytest.mark.parametrize("kind", ["spread", "few"])
+def test_evict_of_very_long_sequences(nb, kind, N, lengths):
+    """Sequences of more pieces than there are workgroups for, up to and beyond the first such length."""
+    B, H, D, block, keep = len(lengths), 2, 64, 64, 40000
+    rng = np.random.default_rng(N)
+    w = rng.uniform(0, 1, (B, H, N)).astype(np.float32) if kind == "spread" else rng.integers(0, 9, (B, H, N)).astype(np.float32)
+    k = torch.arange(N, device="cuda", dtype=torch.int32)[:, None].bitwise_right_shift(torch.arange(D, device="cuda", dtype=torch.int32) % 24) % 100
+    k = k.to(torch.int8).expand(B, H, N, D)                        # codes that tell tokens apart
+    scale = torch.ones((B, H, N // block), device="cuda")
+    v = torch.empty((N, D), device="cuda", dtype=torch.int8).copy_(k[0, 0]).neg_().expand(B, H, N, D)
+    to = nb.kv_cache_empty(B, H, -(-keep // block) * block, D, block)
+    kept, w_out, left = nb.kv_cache_evict(nb.kv_cache(k, v, scale, scale.clone()), to, dev(w), i32(lengths), keep, n_global=5, n_recent=300)
+    assert left.tolist() == [min(n, keep) for n in lengths]
+    kept, w_out = kept.cpu().numpy(), w_out.cpu().numpy()
+    for b in range(B):
+        for h in range(H):
+            want = select(w[b, h], lengths[b], keep, 5, 300)
+            n = len(want)
+            assert np.array_equal(kept[b, h, :n], want) and (kept[b, h, n:] == -1).all()
+            assert np.array_equal(w_out[b, h, :n], w[b, h, want]) and not w_out[b, h, n:].any()
+            at = torch.from_numpy(want).cuda()
+            values = oracle.values(f64(to.k[b:b + 1, h:h + 1]), f64(to.k_scale[b:b + 1, h:h + 1]))[0, 0, :n]
+            assert np.array_equal(values, f64(k[b, h][at])) and np.array_equal(f64(to.v[b, h]), -f64(to.k[b, h]))

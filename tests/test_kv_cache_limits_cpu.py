@@ -1,4 +1,5 @@
 """The 8-bit key/value cache at the limits of what its entry points take, without a GPU."""
+import ctypes
 import os
 import subprocess
 
@@ -26,3 +27,13 @@ static_assert(all_good(), "shares");
 """)
     r = subprocess.run([hip_build.HIPCC, "--offload-host-only", "-fsyntax-only", "-std=c++17", str(src)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     assert r.returncode == 0, r.stdout[-2000:]
+
+
+def test_the_selections_scratch_does_not_grow_without_end():
+    """Its histograms are read by every workgroup of the sequence and head: their number has an end."""
+    from paper_2601_12150_amd import binding as nb
+    need = []
+    for capacity in [1 << n for n in range(10, 31)]:
+        c = nb.ns_kv_cache(3, 2, 64, capacity, 64, nb.NS_CODE_I8, 2 * capacity * 64, capacity * 64, 64, 0x10000, 0x20000, 0x30000, 0x40000)
+        need.append(nb.lib.kv_cache_evict_workspace_bytes(ctypes.byref(c), 64))
+    assert need[0] == 0 and need[10] > 0 and max(need) <= 6 * (2 << 20)
