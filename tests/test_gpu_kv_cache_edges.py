@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_kv_cache as base
 from oracle import kv_cache as oracle
 from test_gpu_kv_cache import CODES, DTYPES, check_attention, check_same, dev, f64, i32, make, nb, rounded  # noqa: F401  (nb: the fixture)
 
@@ -273,3 +274,57 @@ def test_evict_of_very_long_sequences(nb, kind, N, lengths):
             at = torch.from_numpy(want).cuda()
             values = oracle.values(f64(to.k[b:b + 1, h:h + 1]), f64(to.k_scale[b:b + 1, h:h + 1]))[0, 0, :n]
             assert np.array_equal(values, f64(k[b, h][at])) and np.array_equal(f64(to.v[b, h]), -f64(to.k[b, h]))
+
+
+# ---- kernels' variants that the sizes of test_gpu_kv_cache.py do not reach
+
+
+@pytest.mark.parametrize("kind", ["spread", "few", "odd"])
+@pytest.mark.parametrize("code,B,H,D,block,N,M,keep,n_global,n_recent,lengths", [
+    ("i8", 2, 1, 64, 64, 8256, 4096, 4000, 1, 0, [8193, 8256]),            # more than 8192 tokens in one workgroup's registers
+    ("e4m3", 4, 1, 64, 32, 16384, 8192, 8192, 4, 100, [16384, 16383, 8193, 8192]),     # as many as it takes
+    ("i8", 3, 1, 64, 32, 16416, 8192, 8001, 4, 100, [16416, 16384, 8192]),   # and more
+    ("e4m3", 2, 2, 128, 128, 640, 384, 300, 1, 0, [640, 401]),             # blocks of 16384 codes
+    ("i8", 2, 1, 256, 64, 640, 320, 257, 0, 5, [640, 300]),
+    ("e4m3", 1, 2, 256, 128, 1280, 640, 600, 3, 70, [1280]),               # and of 32768
+    ("i8", 2, 1, 256, 128, 1280, 640, 513, 3, 70, [1279, 513]),
+])
+def test_evict_of_other_sizes(nb, code, kind, B, H, D, block, N, M, keep, n_global, n_recent, lengths):
+    base.test_evict(nb, code, kind, B, H, D, block, N, M, keep, n_global, n_recent, lengths)
+
+
+@pytest.mark.parametrize("dtype,code,B,H,G,D,block,N,T,lengths,causal", [
+    ("bf16", "i8", 16, 16, 1, 256, 64, 256, 40, None, True),               # 256 channels' weights without rows to share out
+    ("bf16", "e4m3", 8, 16, 1, 256, 32, 544, 40, None, False),
+    ("f32", "e4m3", 16, 16, 1, 256, 32, 160, 40, None, True),
+    ("bf16", "i8", 1, 1, 1, 64, 32, 32, 70, [32], True),                   # many rows of a single block, and of one and a half tiles
+    ("f32", "e4m3", 2, 1, 1, 128, 32, 32, 40, [31, 32], False),
+    ("bf16", "e4m3", 1, 1, 1, 256, 32, 32, 40, [32], True),
+    ("f32", "i8", 1, 1, 2, 256, 32, 96, 40, [95], True),
+    ("bf16", "i8", 1, 2, 1, 128, 32, 96, 70, [96], True),
+])
+def test_attention_of_other_sizes(nb, dtype, code, B, H, G, D, block, N, T, lengths, causal):
+    lengths = [N, 0, 1, N - 1, *np.random.default_rng(B).integers(0, N + 1, B).tolist()][:B] if lengths is None else lengths
+    base.attention_case(nb, dtype, code, B, H, G, D, block, N, T, lengths, None, causal)
+
+
+@pytest.mark.parametrize("D,T,N", [(64, 1, 96), (128, 3, 1024), (64, 90, 640), (256, 33, 512)])
+def test_nothing_is_written_beside_the_log_sums(nb, D, T, N):
+    """lse is asked of the C ABI, between guard bands; what it holds is what the binding returns."""
+    B, H, G, block = 2, 2, 2, 32
+    rng = np.random.default_rng(D)
+    lengths = [N, N // 2]
+    cache, _ = make(nb, rng, B, H, N, D, block, "i8", lengths)
+    q = torch.randn((B, H * G, T, D), device="cuda", dtype=torch.bfloat16)
+    bands, n = base.Bands(), i32(lengths)
+    out, lse = bands((B, H * G, T, D), torch.bfloat16), bands((B, H * G, T), torch.float32)
+    d = nb.ns_kv_attn_desc(H * G, T, nb.NS_BF16, 1, D ** -0.5, *q.stride()[:3], *out.stride()[:3])
+    c = nb.ns_kv_cache(B, H, D, N, block, nb.NS_CODE_I8, *cache.k.stride()[:3], *(t.data_ptr() for t in cache))
+    need = nb.lib.kv_cache_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(d), 0)
+    ws = bands((need,), torch.uint8)
+    torch.cuda.synchronize()
+    assert nb.lib.kv_cache_attn(ctypes.byref(c), ctypes.byref(d), q.data_ptr(), n.data_ptr(), None, out.data_ptr(), lse.data_ptr(), None, None,
+                                ws.data_ptr() if need else None, need, None) == nb.NS_OK
+    bands.check()
+    want = nb.kv_cache_attn(cache, q, n, want_lse=True)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])

@@ -37,3 +37,20 @@ def test_the_selections_scratch_does_not_grow_without_end():
         c = nb.ns_kv_cache(3, 2, 64, capacity, 64, nb.NS_CODE_I8, 2 * capacity * 64, capacity * 64, 64, 0x10000, 0x20000, 0x30000, 0x40000)
         need.append(nb.lib.kv_cache_evict_workspace_bytes(ctypes.byref(c), 64))
     assert need[0] == 0 and need[10] > 0 and max(need) <= 6 * (2 << 20)
+
+
+def test_an_evictions_workspace_is_checked():
+    """A cache of 2^20 tokens needs one."""
+    from paper_2601_12150_amd import binding as nb
+    P = [ctypes.c_void_p(0x10000 * (i + 1)) for i in range(8)]
+    c, to = (nb.ns_kv_cache(1, 2, 64, n, 64, nb.NS_CODE_I8, 2 * n * 64, n * 64, 64) for n in (1 << 20, 128))
+    for i, x in enumerate((c, to)):
+        x.k, x.v, x.k_scale, x.v_scale = (0x10000000 * (4 * i + j + 1) for j in range(4))
+    need = nb.lib.kv_cache_evict_workspace_bytes(ctypes.byref(c), 100)
+    assert need > 0
+
+    def evict(ws, size):
+        return nb.lib.kv_cache_evict(ctypes.byref(c), ctypes.byref(to), P[0], P[1], 100, 1, 2, P[2], P[3], P[4], ws, size, None)
+
+    for ws, size in ((None, 0), (None, need), (P[5], need - 1), (P[5], 0), (ctypes.c_void_p(0x60010), need)):
+        assert evict(ws, size) == nb.NS_ERR_WORKSPACE, (ws, size)
