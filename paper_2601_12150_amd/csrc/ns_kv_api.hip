@@ -48,8 +48,8 @@ ns_status validate_dtype(int dtype) {
 }
 
 ns_status validate_rows(int64_t sb, int64_t sh, int64_t st, int dtype, int D, const char *what) {
-  const int64_t es = elt_size(dtype);
-  if (st < D || sb < 0 || sh < 0 || (sb * es) % 16 || (sh * es) % 16 || (st * es) % 16)
+  const int64_t unit = 16 / elt_size(dtype);
+  if (st < D || sb < 0 || sh < 0 || sb % unit || sh % unit || st % unit)
     return fail(NS_ERR_INVALID_ARG, "%s strides must be non-negative, rows 16-byte aligned, stride_t >= head_dim", what);
   return NS_OK;
 }
