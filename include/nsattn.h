@@ -329,7 +329,8 @@ typedef struct ns_kv_cache {
   int32_t batch;     /* B >= 1 sequences; NS_ERR_UNSUPPORTED above 65535                  */
   int32_t heads_kv;  /* key/value heads; at most 1024                                    */
   int32_t head_dim;  /* D: 64, 128 or 256                                                */
-  int32_t capacity;  /* tokens there is room for: a multiple of block, at most 2^30      */
+  int32_t capacity;  /* tokens there is room for: a multiple of block, at most 2^30 (attention: batch x heads_kv x
+                        (capacity rounded up to 128) below 2^38)                         */
   int32_t block;     /* tokens that share a scale: 32, 64 or 128                         */
   int32_t code;      /* ns_kv_code                                                       */
   int64_t stride_b, stride_h, stride_t; /* strides of k and v in bytes: multiples of 16, not negative, D <= stride_t
@@ -347,7 +348,9 @@ typedef struct ns_kv_cache {
  * Tokens that the capacity has no room for are dropped.  A block that the new tokens enter from its first position on gets
  * the scale they need.  One that holds tokens before start[b] keeps its scale where that suffices for the new tokens (their
  * magnitudes are at most 127 or 448 times the scale); else it gets the one they need, to which the codes before are rounded again.  Other blocks and positions are left as they are.
- * Two calls that enter the same tokens leave the same cache.
+ * Two calls that enter the same tokens leave the same cache.  A caller who takes tokens back (drafts that were not accepted) does so by
+ * its counts alone: their place is entered again later.  What they did to their block stays where it holds older tokens: a larger
+ * scale, with the older codes rounded to it, or NaN for good.
  */
 ns_status kv_cache_append(const ns_kv_cache *cache, int32_t tokens, int32_t dtype, const void *k, const void *v,
                           int64_t stride_b, int64_t stride_h, int64_t stride_t, const int32_t *start,
@@ -375,8 +378,10 @@ ns_status kv_cache_read(const ns_kv_cache *cache, const int32_t *lengths, int32_
  *            plus, for every position, the softmax weights that all queries of the heads that read it give it.  The two may
  *            be the same memory; positions from lengths[b] on are then left as they are.
  * A query that sees nothing (an empty sequence, t >= counts[b]) gets zeros, lse -inf, and gives no weight.
- * Logits, softmax and sums are fp32; the sums over the values hold them times 2^15 at most, and take a head's V scales of up to
- * 2^80, within a factor of 2^120 of each other (blocks of zeros, whose scale is 2^-100 or 0, aside).
+ * Logits, softmax and sums are fp32.  The products take queries to 2^-39 of their row's largest magnitude, and those of fp32 to 2^-23 of
+ * themselves besides; they take the weights that multiply the values to 11 bits in bf16 calls and to 2^-23 of themselves in fp32 calls,
+ * and those far below their row's largest to 2^-36 of that one.  The weights that are handed out, and lse, are as they were before that.
+ * The sums over the values hold them times 2^15 at most, and take a head's V scales of up to 2^80, within a factor of 2^120 of each other (blocks of zeros, whose scale is 2^-100 or 0, aside).
  */
 typedef struct ns_kv_attn_desc {
   int32_t heads;     /* query heads: a multiple of heads_kv, at most 1024; heads * tokens at most 2^24 */
@@ -389,7 +394,9 @@ typedef struct ns_kv_attn_desc {
 } ns_kv_attn_desc;
 
 /* Bytes of workspace (256-byte aligned) a call needs; want_weights: with weights_out.  0 where the call is refused, and
- * where it needs none. */
+ * where it needs none.  With weights_out, up to 10 rows (queries of all the heads that read one key/value head; 16 of 256 channels) keep
+ * their logits there, 4 bytes for each row and position of the capacity, for which the cache has 2 * head_dim bytes; for more rows the
+ * keys are read again instead. */
 size_t kv_cache_attn_workspace_bytes(const ns_kv_cache *cache, const ns_kv_attn_desc *desc, int32_t want_weights);
 ns_status kv_cache_attn(const ns_kv_cache *cache, const ns_kv_attn_desc *desc, const void *q, const int32_t *lengths,
                         const int32_t *counts, void *out, float *lse, const float *weights_in, float *weights_out,
@@ -397,7 +404,7 @@ ns_status kv_cache_attn(const ns_kv_cache *cache, const ns_kv_attn_desc *desc, c
 
 /*
  * Eviction by added-up weight: of every sequence and key/value head, keep tokens stay and move together, in order, into
- * another cache (same batch, heads_kv, head_dim, block and code; room for `keep` tokens at least; memory of its own).
+ * another cache (same batch, heads_kv, head_dim, block and code; room for `keep` tokens at least; memory of its own); 1 <= keep <= from->capacity.
  * A sequence of at most keep tokens stays whole.  Of a longer one stay: the first n_global, the last n_recent
  * (n_global + n_recent <= keep), and of the others those with the largest weights; equal ones (-0 == +0) rank by lower
  * position first, NaN above everything.  Every head has its own choice.

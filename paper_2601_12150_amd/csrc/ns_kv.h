@@ -152,8 +152,8 @@ template <int CODE> __device__ __forceinline__ void kv_frags_t(const uint32_t (&
 }
 
 // ---- queries as fp16.  A row is scaled by a power of two that brings its largest magnitude to 2^14 .. 2^15: what lies 28 binades
-// below it keeps its 11 bits (bf16 has 8; fp32 is taken as the sum of two such numbers, 22 bits), what lies further below is off by at
-// most 2^-39 of the largest.
+// below it keeps its 11 bits (bf16 has 8).  fp32 is taken as the sum of two such numbers, each the nearest, which is off by 2^-23 of the
+// value at most (fp32's own step is 2^-23 of it, or less); what lies 2^-16 below the largest or further is off by at most 2^-39 of the largest.
 __device__ __forceinline__ int kv_row_shift(uint32_t most) { return most >= kInfBits ? 0 : 141 - (int)(most >> 23); }   // q is taken times 2^this
 
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -169,7 +169,8 @@ __device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f3
 __device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
 
 // Weights are 2^(z - m + 11) in fp16, m a logit near the largest so far, which is moved up before they pass 2^15: a weight that is the
-// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.
+// largest one's 2^-25 or more keeps its 11 bits, and below it all are within 2^-36 of the largest.  (Two parts, where the call is in fp32: 2^-23
+// of itself from 2^-13 of the largest on, and 2^-36 of the largest below.)  The sums of the weights take them as they were before that rounding.
 constexpr float kLift = 11.f, kRoom = 15.f;
 
 // positions that query t sees: 0 .. limit - 1

@@ -546,7 +546,11 @@ int rows_of(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return d.heads / c
 
 // Row tiles of 16 that there are registers for
 constexpr int most_tiles(int head_dim) { return head_dim == 256 ? 1 : head_dim == 128 ? 2 : 4; }
-// More rows are a prompt.  Of channels of 64 three and four tiles are bound by the products here, which prompts share out better: 45 us against 33
+// More rows are a prompt: the operands of another tile have no registers here.  Both kernels, 32 heads' 16384 tokens: 16 and 32 rows of 64
+// channels 20 and 23 us against a prompt's 29 and 29, of 128 30 and 35 against 52 and 53, 16 of 256 54 against 128; 8 heads' 8192 tokens 32 rows of
+// 128 20.7 against 21.1 (fp32 19 against 25), 16 of 256 19 against 40.  What this does not tell apart: 17 to 32 rows of very many heads with few
+// tokens each, where a prompt would be faster (512 heads' 512 tokens, 32 rows: 46 against 16 us of 64 channels, 54 against 35 of 128).
+// Of channels of 64 three and four tiles are bound by the products here, which prompts share out better: 45 us against 33
 // for 64 heads' 8192 tokens, 41 against 13 for 256 heads' 512.  Where there are few heads of many tokens this has more workgroups, by which its
 // finer shares win: 19 us against 37 for one head's 65536 tokens, 17 against 20 for 8 heads' 8192, 14 against 16 for 8 heads' 1024.
 bool few_rows(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
@@ -562,7 +566,9 @@ bool by_logits(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return rows_of(
 // A workgroup per sequence and head, which spares the records and their join: where a head's tokens are few (8 heads' 1024 of 64 channels 7.5 us
 // against 9.1 shared out, 2048: 11.1 against 9.2; 512 of 128 channels 8.2 against 9.8, 1024: 11.0 against 9.8), and where there is one
 // for every CU (256 heads' 4096 of 128 channels 43.5 against 49.8; of more tokens, still 98.5 against 104.9 for 8192, a single long sequence
-// among short ones would have its heads' workgroups run alone for too long).
+// among short ones would have its heads' workgroups run alone for too long).  That is so below as well, and is what shared capacities of 32
+// sequences cost where their lengths are that far apart: 8 heads of 128 channels, all 4096 tokens long 43 us against 50 shared out, all 2048
+// 24 against 30, all 102 6 against 12, but one of 4096 among 31 of 102 28 against 13 (256 channels: 94 and 102, 44 and 52, 7 and 14, 58 and 19).
 bool alone(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
   return rows_of(c, d) <= 16 && ((int64_t)c.capacity * c.head_dim <= 65536 || (c.capacity <= 4096 && (int64_t)c.batch * c.heads_kv >= device_cu_count()));
 }

@@ -10,7 +10,7 @@
 // Rows are numbered r = token * group + head, so that a causal row tile ends after few more keys than it begins with.
 //
 // Measured: two sequences' 6627 prompt tokens, 32 query heads of 128 channels on 8, bf16 and int8: 240 us, 790 TFLOP/s (512 queries behind
-// 32768 tokens 890 to 930; fp32 590); 512 queries of 16 heads of 64 channels across 16385 tokens 61 us, 280 TFLOP/s.  A tile of 64 keys
+// 32768 tokens 890 to 930; fp32 590), which is what call after call settles at: the first 50 or so after a pause take 270 to 305; 512 queries of 16 heads of 64 channels across 16385 tokens 61 us, 280 TFLOP/s.  A tile of 64 keys
 // by 32 rows of 128 channels is 1024 cycles of products, 512 of exponentials, about 1000 of other vector instructions and 256 of LDS reads of
 // the CU's 2048 for its eight waves: no one of them alone is the bound.
 #include "ns_kv.h"
@@ -847,7 +847,9 @@ ns_status weights_sum(const KvAttnArgs &a, const Frag *frags, const float *facto
     return go(kv_weights_stream_kernel<PARTS, CODE, 128, 2>);
   }
   // a wave has the operands of 64 keys, or 32, in registers.  Its workgroup the same ones, with the rows shared out, where there are fewer
-  // than CUs of workgroups with keys of their own (16 heads of 64, 576 rows and keys, all of the call: 35 -> 27 us; 2048 rows, 320 keys: 65 -> 36)
+  // than CUs of workgroups with keys of their own (16 heads of 64, 576 rows and keys, all of the call: 35 -> 27 us; 2048 rows, 320 keys: 65 -> 36).
+  // Around that border, 512 rows of 16 heads of 64, 128 and 256 channels, all of the call: 240 workgroups 43, 54, 113 us, shared 40, 55, 112; 256 of them
+  // 42, 55, 117 and 39, 56, 117; 512 of them 55, 75, 173 and 57, 82, 193; 1040 of them 93, 131, 318 and 95, 140, 348
   constexpr int KX256 = PARTS == 2 ? 2 : 4;
   const int most = a.c.head_dim == 256 ? 64 * KX256 : 256;
   const bool share = (int64_t)((a.c.capacity + most - 1) / most) * a.c.heads_kv * a.c.batch < device_cu_count();
