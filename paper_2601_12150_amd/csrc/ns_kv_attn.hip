@@ -327,19 +327,19 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
         float z[8], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; i++) z[i] = __builtin_fmaf(s[i / 4][i % 4], f, -ref);
-        svr[nt] = sv;
+        svr[nt] = sv * (1.f / Lift<true>::factor);
         if (edge) {
           asm volatile("; edge");
 #pragma unroll
           for (int i = 0; i < 8; i++) z[i] = n0 + (i / 4) * 16 + 4 * g + i % 4 < limit[nt] ? z[i] : -INFINITY;
-          svr[nt] = n0 >= limit[nt] ? 0.f : sv;                                        // a NaN block is NaN for those who see it
+          svr[nt] = n0 >= limit[nt] ? 0.f : svr[nt];                                   // a NaN block is NaN for those who see it
         }
 #pragma unroll
         for (int i = 0; i < 8; i++) top = fmaxf(top, z[i]);
-        if (__any(top > kRoom || (fresh && top > -INFINITY))) {
+        if (__any(top > Lift<true>::room || (fresh && top > -INFINITY))) {
           top = half_swap_max(row_swap_max(top));
-          const bool moved = top > kRoom || (fresh && top > -INFINITY);
-          const float move = moved ? top - kLift : 0.f;
+          const bool moved = top > Lift<true>::room || (fresh && top > -INFINITY);
+          const float move = moved ? top : 0.f;
           // (a fresh row's sums are 0, or NaN: not times a factor beyond fp32 where its logits are far below 0)
           const float fade = __builtin_amdgcn_exp2f(fminf(-move, 0.f));
 #pragma unroll
@@ -354,6 +354,7 @@ void kv_attn_split_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const in
         for (int i = 0; i < 8; i++) {
           p[i] = __builtin_amdgcn_exp2f(z[i]);
           l[nt] += p[i];
+          p[i] *= Lift<true>::factor;
         }
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {

@@ -56,6 +56,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
   constexpr uint32_t kV = kKeys * D * 2, kHalf = kV + kKeys * DV * 2;   // bytes of a tile's K, and with its V^T
   // Registers for both parts of the queries, and LDS for two tiles?  fp32 with D = 256 has the second part in LDS, and one tile.
   constexpr bool EARLY = PARTS * D < 512;
+  using L = Lift<PARTS == 2>;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
@@ -305,10 +306,10 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     for (int x = 0; x < 2; x++)
 #pragma unroll
       for (int e = 0; e < 16; e++) top = fmaxf(top, s[x][e]);
-    if (__any(top > kRoom || (fresh && top > -INFINITY)) || tile_unit != unit) {
+    if (__any(top > L::room || (fresh && top > -INFINITY)) || tile_unit != unit) {
       top = half_swap_max(top);
-      const bool moved = top > kRoom || (fresh && top > -INFINITY);
-      const float move = moved ? top - kLift : 0.f;
+      const bool moved = top > L::room || (fresh && top > -INFINITY);
+      const float move = moved ? top - L::exponent : 0.f;
       float fade = __builtin_amdgcn_exp2f(fminf(-move, 0.f));      // (a fresh row's sums are 0, or NaN: not times a factor beyond fp32)
 #pragma unroll
       for (int x = 0; x < 2; x++)
@@ -327,10 +328,12 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     for (int x = 0; x < 2; x++)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[x][e]), p1 = __builtin_amdgcn_exp2f(s[x][e + 1]);
-        const uint32_t hi = pack_f16(p0, p1);
+        float p0 = __builtin_amdgcn_exp2f(s[x][e]), p1 = __builtin_amdgcn_exp2f(s[x][e + 1]);
         ls[e % 4] += p0;
         ls[e % 4 + 1] += p1;
+        p0 *= L::factor;
+        p1 *= L::factor;
+        const uint32_t hi = pack_f16(p0, p1);
         pf[0][x * 2 + e / 8].w[e % 8 / 2] = hi;
         if (PARTS == 2) {
           const f16x2 w = __builtin_bit_cast(f16x2, hi);
@@ -426,7 +429,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
   if (!real) return;
   if (a.splits > 1) {
     const int64_t rec = ((int64_t)split * c.batch * c.heads_kv + row) * R + r;
-    const float u = unit;
+    const float u = unit * (1.f / L::factor);
 #pragma unroll
     for (int i = 0; i < MT; i++)
 #pragma unroll
@@ -436,7 +439,7 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
     return;
   }
   const bool some = m != -INFINITY;
-  const float by = some ? unit / l : 0.f;
+  const float by = some ? unit / (l * L::factor) : 0.f;
   T *to = out + b * d.out_stride_b + (int64_t)hq * d.out_stride_h + (int64_t)t * d.out_stride_t + part * DV;
 #pragma unroll
   for (int i = 0; i < MT; i++)

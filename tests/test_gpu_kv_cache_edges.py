@@ -328,3 +328,36 @@ def test_nothing_is_written_beside_the_log_sums(nb, D, T, N):
     bands.check()
     want = nb.kv_cache_attn(cache, q, n, want_lse=True)
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("T", [1, 70])
+@pytest.mark.parametrize("dtype,code,D,N", [("bf16", "i8", 64, 32), ("f32", "e4m3", 128, 64), ("bf16", "e4m3", 128, 2048), ("f32", "i8", 256, 64), ("bf16", "i8", 256, 2048)])
+def test_log_sums_of_few_keys_with_small_logits(nb, dtype, code, D, N, T):
+    """Rows of one channel, whose logits are single products: z is off by the scaling's four roundings.  One key's log-sum is its logit and
+    its weight is 1; that of n equal keys is log n more, its weights 1 / n.  Roundings behind z: the sum's (a whole number, exact), the
+    logarithm's and the two that put z and it together, 2^-24 each of the larger one (the instruction's: 2^-23); the weight's exponent twice
+    that, its exponential 2^-23.  bf16 calls of many rows have exponents that are 11 higher, in steps of 2^-20: half of one for the weight, and
+    one for the sum's logarithm, times log 2, are 2^-20 more of the log-sum and twice that of the weights.  In the fp32 calls out is the value to the weight's two parts (2^-23) and the normalisation (2^-23)."""
+    n = 5 if T == 1 else 3
+    B, H, block = n, 1, 32
+    codes = torch.zeros((B, H, N, D)).to(CODES[code])
+    codes[..., 0] = torch.full((B, H, N), 96.0).to(CODES[code])
+    codes = codes.cuda()
+    scale = torch.full((B, H, N // block), 2.0 ** -9, device="cuda")
+    cache = nb.kv_cache(codes, codes.clone(), scale, scale.clone())
+    q = np.zeros((B, H, T, D))
+    q[..., 0] = np.random.default_rng(D).uniform(-9, 9, (B, H, T))
+    q = rounded(q.astype(np.float32), dtype)
+    lengths = list(range(1, n + 1))
+    out, lse, weights = nb.kv_cache_attn(cache, dev(q, DTYPES[dtype]), i32(lengths), scale=0.1, causal=False, want_lse=True, want_weights=True)
+    z = float(np.float32(0.1)) * q[..., 0] * 96 * 2.0 ** -9
+    many = np.array(lengths)[:, None, None]
+    want, size = z + np.log(many), np.maximum(np.abs(z), np.log(many))
+    more = 2.0 ** -20 if dtype == "bf16" and T == 70 else 0.0
+    assert (np.abs(f64(lse) - want) <= more + 4 * 2.0 ** -24 * np.abs(z) + 4 * 2.0 ** -24 * np.maximum(size, np.abs(want))).all()
+    step = 2 * (8 * 2.0 ** -24 * np.maximum(size, np.abs(want))).max() + 2.0 ** -23 + 2 * more
+    for b in range(B):
+        assert np.abs(f64(weights)[b, 0, :lengths[b]] * lengths[b] / T - 1).max() <= step + T * 2.0 ** -24
+        assert not f64(weights)[b, 0, lengths[b]:].any()
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    assert np.abs(f64(out)[..., 0] / (96 * 2.0 ** -9) - 1).max() <= 2.0 ** -22 + half and not f64(out)[..., 1:].any()
