@@ -381,8 +381,8 @@ ns_status kv_cache_read(const ns_kv_cache *cache, const int32_t *lengths, int32_
  * Logits, softmax and sums are fp32.  The products take queries to 2^-39 of their row's largest magnitude, and those of fp32 to 2^-23 of
  * themselves besides; they take the weights that multiply the values to 11 bits in bf16 calls and to 2^-23 of themselves in fp32 calls,
  * and those far below their row's largest to 2^-36 of that one.  The weights that are handed out, and lse, are as they were before that;
- * lse of bf16 calls of many rows (more than 32 of a key/value head, 16 of 256 channels) is off by up to 2^-20 whatever its size, and those
- * weights by up to 2^-19 of themselves.
+ * in bf16 calls of many rows (more than 32 of a key/value head, 16 of 256 channels) to a capacity above 512 lse is off by up to 2^-20
+ * whatever its size, and those weights by up to 2^-19 of themselves.
  * The sums over the values hold them times 2^15 at most, and take a head's V scales of up to 2^80, within a factor of 2^120 of
  * each other (blocks of zeros, whose scale is 2^-100 or 0, aside).
  */

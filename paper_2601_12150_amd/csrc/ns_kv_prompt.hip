@@ -49,14 +49,15 @@ struct PromptArgs {
 
 // Item x: a tile of rows of a head, or its part of the keys.
 // DV: channels of V, and of out, that a workgroup takes: all, or half of them (fp32, D = 256: registers; the logits are computed twice)
-template <typename T, int CODE, int D, int DV, int WAVES>
+// FACTOR: as Lift has it
+template <typename T, int CODE, int D, int DV, int WAVES, bool FACTOR>
 __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv_attn_desc &d, const T *q, const int32_t *lengths, const int32_t *counts,
                                                T *out, float *lse, const PromptArgs &a, int x) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1, KS = D / 16, MT = DV / 32, ROWS = WAVES * 32, THREADS = WAVES * 64;
   constexpr uint32_t kV = kKeys * D * 2, kHalf = kV + kKeys * DV * 2;   // bytes of a tile's K, and with its V^T
   // Registers for both parts of the queries, and LDS for two tiles?  fp32 with D = 256 has the second part in LDS, and one tile.
   constexpr bool EARLY = PARTS * D < 512;
-  using L = Lift<PARTS == 2>;
+  using L = Lift<FACTOR>;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
@@ -461,14 +462,14 @@ __device__ __forceinline__ void kv_prompt_item(const ns_kv_cache &c, const ns_kv
 // Workgroups that are through with an item draw the next one.  Dealt out by the hardware, which hands workgroups to the shader engines
 // in turn, whether or not another one has room, items of very different lengths (a padded batch, causal rows) kept a third of the CUs
 // waiting: 293 us for the prompts of 2 x 4096 tokens that take 262 us drawn (245 us with the operands' reads ahead).
-template <typename T, int CODE, int D, int DV, int WAVES>
+template <typename T, int CODE, int D, int DV, int WAVES, bool FACTOR>
 __global__ __launch_bounds__(WAVES * 64, D > 128 ? 1 : D == 64 && sizeof(T) == 2 ? 3 : 2)
 void kv_prompt_kernel(ns_kv_cache c, ns_kv_attn_desc d, const T *q, const int32_t *lengths, const int32_t *counts, T *out, float *lse, PromptArgs a) {
   __shared__ int drawn;
   int x = (int)blockIdx.x;
   while (true) {
     if (threadIdx.x == 0 && a.tickets) drawn = (int)gridDim.x + atomicAdd(a.tickets, 1);
-    kv_prompt_item<T, CODE, D, DV, WAVES>(c, d, q, lengths, counts, out, lse, a, x);
+    kv_prompt_item<T, CODE, D, DV, WAVES, FACTOR>(c, d, q, lengths, counts, out, lse, a, x);
     if (!a.tickets) return;
     __syncthreads();
     x = drawn;
@@ -786,7 +787,7 @@ Layout layout_of(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) {
   return w;
 }
 
-template <typename T, int CODE, int D>
+template <typename T, int CODE, int D, bool FACTOR>
 ns_status launch(const KvAttnArgs &a) {
   constexpr int WAVES = waves_of(D), DV = sizeof(T) == 4 && D == 256 ? 128 : D;
   const ns_kv_cache &c = a.c;
@@ -798,7 +799,7 @@ ns_status launch(const KvAttnArgs &a) {
   const int tile_lds = kKeys * (D + DV) * 2, lds = DV == D ? 2 * tile_lds : tile_lds + WAVES * 32 * D * 2;
   const T *q = static_cast<const T *>(a.q);
   T *out = static_cast<T *>(a.out);
-  ns_status st = reserve_lds_once(reinterpret_cast<const void *>(kv_prompt_kernel<T, CODE, D, DV, WAVES>), lds);
+  ns_status st = reserve_lds_once(reinterpret_cast<const void *>(kv_prompt_kernel<T, CODE, D, DV, WAVES, FACTOR>), lds);
   if (st != NS_OK) return st;
   const int64_t items = (int64_t)tiles * w.splits * (D / DV) * c.heads_kv * c.batch;
   if (items > 0x7fffffff - 65536) return fail(NS_ERR_UNSUPPORTED, "too many rows");
@@ -809,7 +810,7 @@ ns_status launch(const KvAttnArgs &a) {
     hipLaunchKernelGGL(kv_no_tickets_kernel, dim3(1), dim3(1), 0, a.stream, p.tickets);
     if ((st = check_launch("kv_no_tickets_kernel")) != NS_OK) return st;
   }
-  hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES>), dim3((unsigned)workgroups), dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out,
+  hipLaunchKernelGGL((kv_prompt_kernel<T, CODE, D, DV, WAVES, FACTOR>), dim3((unsigned)workgroups), dim3(WAVES * 64), lds, a.stream, c, a.d, q, a.lengths, a.counts, out,
                      a.lse, p);
   st = check_launch("kv_prompt_kernel");
   Frag *frags = reinterpret_cast<Frag *>(a.ws + w.frags);
@@ -824,8 +825,13 @@ ns_status launch(const KvAttnArgs &a) {
   return launch_kv_weights_again(a, frags, factors, p.lse2, w.splits == 1);
 }
 
-template <typename T, int CODE> ns_status launch_d(const KvAttnArgs &a) {
-  return a.c.head_dim == 64 ? launch<T, CODE, 64>(a) : a.c.head_dim == 128 ? launch<T, CODE, 128>(a) : launch<T, CODE, 256>(a);
+template <typename T, int CODE, bool FACTOR> ns_status launch_d(const KvAttnArgs &a) {
+  return a.c.head_dim == 64 ? launch<T, CODE, 64, FACTOR>(a) : a.c.head_dim == 128 ? launch<T, CODE, 128, FACTOR>(a) : launch<T, CODE, 256, FACTOR>(a);
+}
+template <typename T, int CODE> ns_status launch_any(const KvAttnArgs &a) {
+  if constexpr (sizeof(T) == 2)
+    if (a.c.capacity > kFewKeys) return launch_d<T, CODE, false>(a);
+  return launch_d<T, CODE, true>(a);
 }
 
 template <int PARTS, int CODE>
@@ -888,8 +894,8 @@ ns_status launch_kv_weights_again(const KvAttnArgs &a, Frag *frags, float *facto
 size_t kv_prompt_workspace_bytes(const ns_kv_cache &c, const ns_kv_attn_desc &d, bool weights) { return layout_of(c, d, weights).total; }
 
 ns_status launch_kv_prompt(const KvAttnArgs &a) {
-  if (a.d.dtype == NS_F32) return a.c.code == NS_CODE_I8 ? launch_d<float, NS_CODE_I8>(a) : launch_d<float, NS_CODE_E4M3>(a);
-  return a.c.code == NS_CODE_I8 ? launch_d<bf16_t, NS_CODE_I8>(a) : launch_d<bf16_t, NS_CODE_E4M3>(a);
+  if (a.d.dtype == NS_F32) return a.c.code == NS_CODE_I8 ? launch_any<float, NS_CODE_I8>(a) : launch_any<float, NS_CODE_E4M3>(a);
+  return a.c.code == NS_CODE_I8 ? launch_any<bf16_t, NS_CODE_I8>(a) : launch_any<bf16_t, NS_CODE_E4M3>(a);
 }
 
 }  // namespace ns

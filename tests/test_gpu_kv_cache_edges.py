@@ -336,7 +336,7 @@ def test_log_sums_of_few_keys_with_small_logits(nb, dtype, code, D, N, T):
     """Rows of one channel, whose logits are single products: z is off by the scaling's four roundings.  One key's log-sum is its logit and
     its weight is 1; that of n equal keys is log n more, its weights 1 / n.  Roundings behind z: the sum's (a whole number, exact), the
     logarithm's and the two that put z and it together, 2^-24 each of the larger one (the instruction's: 2^-23); the weight's exponent twice
-    that, its exponential 2^-23.  bf16 calls of many rows have exponents that are 11 higher, in steps of 2^-20: half of one for the weight, and
+    that, its exponential 2^-23.  bf16 calls of many rows in caches of more than 512 tokens have exponents that are 11 higher, in steps of 2^-20: half of one for the weight, and
     one for the sum's logarithm, times log 2, are 2^-20 more of the log-sum and twice that of the weights.  In the fp32 calls out is the value to the weight's two parts (2^-23) and the normalisation (2^-23)."""
     n = 5 if T == 1 else 3
     B, H, block = n, 1, 32
@@ -353,7 +353,7 @@ def test_log_sums_of_few_keys_with_small_logits(nb, dtype, code, D, N, T):
     z = float(np.float32(0.1)) * q[..., 0] * 96 * 2.0 ** -9
     many = np.array(lengths)[:, None, None]
     want, size = z + np.log(many), np.maximum(np.abs(z), np.log(many))
-    more = 2.0 ** -20 if dtype == "bf16" and T == 70 else 0.0
+    more = 2.0 ** -20 if dtype == "bf16" and T == 70 and N > 512 else 0.0
     assert (np.abs(f64(lse) - want) <= more + 4 * 2.0 ** -24 * np.abs(z) + 4 * 2.0 ** -24 * np.maximum(size, np.abs(want))).all()
     step = 2 * (8 * 2.0 ** -24 * np.maximum(size, np.abs(want))).max() + 2.0 ** -23 + 2 * more
     for b in range(B):
