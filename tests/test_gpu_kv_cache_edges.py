@@ -361,3 +361,44 @@ def test_log_sums_of_few_keys_with_small_logits(nb, dtype, code, D, N, T):
         assert not f64(weights)[b, 0, lengths[b]:].any()
     half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
     assert np.abs(f64(out)[..., 0] / (96 * 2.0 ** -9) - 1).max() <= 2.0 ** -22 + half and not f64(out)[..., 1:].any()
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_from_the_backbone_into_the_cache(nb, code):
+    """What a reader behind the backbone calls: the stack prunes, linear maps make keys and values of the tokens it kept, these enter a cache
+    as views of the map's output, queries attend across them with weights, and the tokens with the least weight leave.  The oracle of the cache
+    starts from what the maps wrote."""
+    from paper_2601_12150_amd import synth
+    from test_gpu_vit_block import dev_weights
+    B, g, heads, dim, keep_k, H, G, D, block, T = 2, 16, 8, 512, 150, 2, 2, 128, 32, 40
+    rng = np.random.default_rng(30)
+    x = dev(synth.round_to_bf16(rng.standard_normal((B, 1 + g * g, dim)).astype(np.float32)), torch.bfloat16)
+    tokens, kept = nb.vit_forward(x, [dev_weights(synth.make_block_weights(dim, dim, seed=40 + i)) for i in range(2)], g, g, 8, heads, prune_after=1, keep_k=keep_k)
+    n = 1 + keep_k
+    w = dev(synth.round_to_bf16((rng.standard_normal((2 * H * D, dim)) * dim ** -0.5).astype(np.float32)), torch.bfloat16)
+    kv = nb.linear_forward(tokens.view(B * n, dim), w, torch.zeros(2 * H * D, device="cuda")).view(B, n, 2, H, D)
+    k, v = (kv[:, :, i].transpose(1, 2) for i in range(2))
+    N = 192
+    cache = nb.kv_cache_empty(B, H, N, D, block, CODES[code])
+    nb.kv_cache_append(cache, k, v, i32([0] * B))
+    host = [np.zeros((B, H, N, D)), np.ones((B, H, N // block)), np.zeros((B, H, N, D)), np.ones((B, H, N // block))]
+    for i, t in ((0, k), (2, v)):
+        oracle.append(host[i], host[i + 1], f64(t), [0] * B, [n] * B, code)
+    check_same(cache, host)
+    q = dev(rounded(rng.standard_normal((B, H * G, T, D)).astype(np.float32), "bf16"), torch.bfloat16)
+    out, lse, weights = nb.kv_cache_attn(cache, q, i32([n] * B), causal=False, want_lse=True, want_weights=True)
+    want = oracle.attend(f64(q), oracle.values(host[0], host[1]), oracle.values(host[2], host[3]), [n] * B, [T] * B, float(np.float32(D ** -0.5)), False)
+    check_attention(out, lse, weights, want, "bf16", D, N, G * T)
+    to = nb.kv_cache_empty(B, H, 96, D, block, CODES[code])
+    chosen, moved, left = nb.kv_cache_evict(cache, to, weights, i32([n] * B), 90)
+    assert left.tolist() == [90] * B and (chosen[:, :, 0] == 0).all()              # (the CLS token stays)
+    for b in range(B):
+        for h in range(H):
+            at = oracle.select(weights[b, h].cpu().numpy(), n, 90, 1, 0)
+            assert np.array_equal(chosen[b, h].cpu().numpy(), at) and torch.equal(moved[b, h, :90], weights[b, h][chosen[b, h].long()])
+            # the patches that they are, in the image
+            patches = kept[b][chosen[b, h, 1:].long() - 1]
+            assert (patches[1:] > patches[:-1]).all()
+            for codes, scale, i in ((to.k, to.k_scale, 0), (to.v, to.v_scale, 2)):
+                ref, ref_scale = oracle.move(host[i][b, h], host[i + 1][b, h], at, block, code)
+                assert np.array_equal(f64(codes[b, h]), ref) and np.array_equal(f64(scale[b, h]), ref_scale)
