@@ -318,7 +318,8 @@ ns_status vit_embed(int32_t batch, int32_t channels, int32_t grid_h, int32_t gri
  * Codes are int8 (-127..127) or OCP e4m3 (no NaN).  The scales that the library writes are powers of two: the smallest s of at least
  * 2^-100 with max |x| <= 127 s (e4m3: 448 s) over the block's tokens.  So x / s is exact, codes are the nearest ones to x / s
  * (ties to even), and every value has at most 8 significant bits (exact in bf16).  Scales that the caller writes may be any
- * floats from 2^-100 to 2^80, or 0: its block's values are zeros, whatever the codes.  A NaN scale stands for a block that was given a NaN or an infinity: all its tokens' values are NaN.
+ * floats from 2^-100 to 2^80, or 0: its block's values are zeros, whatever the codes.  A NaN scale stands for a block that was given
+ * a NaN or an infinity: all its tokens' values are NaN.
  *
  * Tokens are in order: position n is token n of the sequence, 0 <= n < its length.  What lies behind a sequence's length is
  * never used, whatever it is.

@@ -567,9 +567,9 @@ bool by_logits(const ns_kv_cache &c, const ns_kv_attn_desc &d) { return rows_of(
 // A workgroup per sequence and head, which spares the records and their join: where a head's tokens are few (8 heads' 1024 of 64 channels 7.5 us
 // against 9.1 shared out, 2048: 11.1 against 9.2; 512 of 128 channels 8.2 against 9.8, 1024: 11.0 against 9.8), and where there is one
 // for every CU (256 heads' 4096 of 128 channels 43.5 against 49.8; of more tokens, still 98.5 against 104.9 for 8192, a single long sequence
-// among short ones would have its heads' workgroups run alone for too long).  That is so below as well, and is what shared capacities of 32
-// sequences cost where their lengths are that far apart: 8 heads of 128 channels, all 4096 tokens long 43 us against 50 shared out, all 2048
-// 24 against 30, all 102 6 against 12, but one of 4096 among 31 of 102 28 against 13 (256 channels: 94 and 102, 44 and 52, 7 and 14, 58 and 19).
+// among short ones would have its heads' workgroups run alone for too long).  That happens with room for 4096 as well, where the lengths are
+// that far apart: 32 sequences' 8 heads of 128 channels, all 4096 tokens long 43 us against 50 shared out, all 2048 24 against 30, all 102 6
+// against 12, but one of 4096 among 31 of 102 28 against 13 (256 channels: 94 and 102, 44 and 52, 7 and 14, 58 and 19).
 bool alone(const ns_kv_cache &c, const ns_kv_attn_desc &d) {
   return rows_of(c, d) <= 16 && ((int64_t)c.capacity * c.head_dim <= 65536 || (c.capacity <= 4096 && (int64_t)c.batch * c.heads_kv >= device_cu_count()));
 }

@@ -10,7 +10,8 @@
 // Rows are numbered r = token * group + head, so that a causal row tile ends after few more keys than it begins with.
 //
 // Measured: two sequences' 6627 prompt tokens, 32 query heads of 128 channels on 8, bf16 and int8: 240 us, 790 TFLOP/s (512 queries behind
-// 32768 tokens 890 to 930; fp32 590), which is what call after call settles at: the first 50 or so after a pause take 270 to 305; 512 queries of 16 heads of 64 channels across 16385 tokens 61 us, 280 TFLOP/s.  A tile of 64 keys
+// 32768 tokens 890 to 930; fp32 590), which is what call after call settles at, the first 50 or so after a pause taking 270 to 305; 512 queries
+// of 16 heads of 64 channels across 16385 tokens 61 us, 280 TFLOP/s.  A tile of 64 keys
 // by 32 rows of 128 channels is 1024 cycles of products, 512 of exponentials, about 1000 of other vector instructions and 256 of LDS reads of
 // the CU's 2048 for its eight waves: no one of them alone is the bound.
 #include "ns_kv.h"
